@@ -46,8 +46,8 @@
  *     Decoding layer by layer in this mode: enqueue kvzap_decode_attention directly behind kvzap_decode_step of
  *     the same layers, where the queries are there by then.  The attention then runs beside the step; with a
  *     kernel of the caller between the two (which is safe) it cannot, and takes a few microseconds longer.
- *   - Stream capture (CUDA graphs): kvzap_decode_step(_fp8) and kvzap_decode_attention(_fp8) may be captured
- *     and replayed.  The other calls rotate scratch sets and counters on the host from call to call and must
+ *   - Stream capture (CUDA graphs): kvzap_decode_step(_fp8), kvzap_decode_attention(_fp8), kvzap_decode_attention_shared
+ *     and kvzap_rotary may be captured and replayed.  The other calls rotate scratch sets and counters on the host from call to call and must
  *     be enqueued, not captured.
  *   - Errors the host can see (bad argument, unsupported shape) return at once
  *     and launch nothing.  Conditions only the device can see set a status
@@ -369,6 +369,60 @@ kvzap_status kvzap_prefill_plan(kvzap_ctx *ctx, int32_t layer, const void *hidde
                                 void *stream);
 
 /*
+ * Rotary positions.  Keys are cached with their positions applied and queries come to the attention with theirs (the paper
+ * takes both from the model; this is the step between its projections and the calls here).  kvzap_set_rotary sets the
+ * frequencies of a context, at any time, on the host:
+ *   pair i of a head's first rotary_dim elements turns by position * f_i:  f_i = inv_freq[i] if given (HOST, [rotary_dim / 2]), else
+ *   base^(-2 i / rotary_dim), in either case scaled for a longer context:
+ *     f_i' = f_i (keep_i + (1 - keep_i) / factor),
+ *     original_context = 0: keep_i = 0 (all frequencies alike; factor = 1 scales nothing)
+ *     original_context > 0: keep_i = clamp((original_context f_i / 2 pi - low) / (high - low), 0, 1): pairs that turn less than `low`
+ *                           times in the original context are scaled, those of more than `high` turns are not, in between in part
+ *   interleaved = 0: pair i is elements (i, i + rotary_dim / 2);  1: elements (2i, 2i + 1)
+ *   magnitude: factor of the rotated elements (both of query and key: logits take its square), 1 for none
+ */
+typedef struct {
+    int32_t head_dim;         /* elements per head of the tensors: multiple of 8, 8..1024                   */
+    int32_t rotary_dim;       /* even, 2..head_dim; the elements behind are left as they are                */
+    int32_t interleaved;
+    float magnitude;
+    double base;              /* > 1                                                                        */
+    double factor;            /* >= 1                                                                       */
+    double original_context;  /* tokens, or 0                                                               */
+    double low, high;         /* turns, 0 <= low < high; unused if original_context = 0                     */
+    const double *inv_freq;   /* NULL, or rotary_dim / 2 frequencies (radians per token, >= 0)              */
+} kvzap_rotary_config;
+kvzap_status kvzap_set_rotary(kvzap_ctx *ctx, const kvzap_rotary_config *cfg);
+
+/* Rows of one tensor: (token t, head h) begins at element t * token + h * head of `in` / `out`, its elements are contiguous. */
+#define KVZAP_ROWS_ROTATE 1   /* rotated; without it the rows are only moved (values)                           */
+#define KVZAP_ROWS_8BIT   2   /* written as 8-bit rows: D E4M3 codes, fp32 scale, 12 zero bytes (kvzap_decode_attention_fp8) */
+typedef struct {
+    const void *in;           /* bf16 (device)                                                              */
+    void *out;                /* bf16, or bytes for 8-bit rows (device)                                     */
+    int64_t in_token, in_head;      /* strides in elements                                                  */
+    int64_t out_token, out_head;    /* strides in elements; in bytes for 8-bit rows                         */
+    int32_t n_heads;
+    uint32_t flags;
+} kvzap_rows;
+
+/*
+ * One launch over up to three tensors of the same tokens, usually queries, keys and values as a fused projection leaves them:
+ *   y1 = (x1 cos - x2 sin) magnitude,  y2 = (x2 cos + x1 sin) magnitude   for pairs of the first rotary_dim elements
+ * with the angle of the token's position, exact at any of them (int32, negative ones turn backwards).  inverse = 1 turns the other way
+ * (what undoes a rotation of magnitude 1, and in any case its gradient).  Rounded once, to bf16 or to codes: scale = the row's largest
+ * magnitude / 448 (1 for zeros), codes = E4M3(x / scale) to nearest.
+ *   positions [n_tokens] int32 (device);  tensors [n_tensors] (HOST, read before return)
+ * Strides give any layout: [T, H, D] inside a wider row in, [H, T, D] out as the pruning calls take K and V.  `out` may be `in` with the
+ * same strides (bf16); otherwise outputs overlap no input.  head_dim and rotary_dim that are multiples of 16, with everything
+ * 16-byte aligned, take the fast path; 8-bit rows need it (head_dim 64 or 128) and 16-byte aligned outputs.
+ * The kernel waits for all work ahead of it in the stream and lets none behind it start early: in either mode of a context it
+ * counts as an ordinary producer of the next call's inputs.
+ */
+kvzap_status kvzap_rotary(kvzap_ctx *ctx, const int32_t *positions, int64_t n_tokens, const kvzap_rows *tensors,
+                          int32_t n_tensors, int32_t inverse, void *stream);
+
+/*
  * Decode-time cache (caption of Algorithm 1: decoding is like prefilling but
  * needs a buffer of scores to enforce the sliding window; contributions:
  * delayed eviction with a sliding window).  One list per (sequence, layer, KV
@@ -469,10 +523,68 @@ kvzap_status kvzap_decode_attention_fp8(kvzap_ctx *ctx, kvzap_cache *cache, int3
  * allocator, which hands released pages out again (to any list) before it touches never-used pages
  * of the pool.  Until the slot is given a new prompt (kvzap_prefill_to_cache) decode steps leave its
  * lists alone (its rows of hidden, K_new, V_new are ignored, its scores still computed) and attention over
- * it gives zeros.  Enqueued on the stream like every other call; the paper does not discuss this, it is
+ * it gives zeros.  Pages that forked sequences hold too (kvzap_cache_fork) stay theirs until the last of them is
+ * released.  Enqueued on the stream like every other call; the paper does not discuss this, it is
  * bookkeeping a serving loop needs around the method.
  */
 kvzap_status kvzap_cache_release_seq(kvzap_cache *cache, int32_t seq, void *stream);
+
+/*
+ * Sequences become copies of others (beams, several samples of one prompt, a prompt kept for later ones; the paper does
+ * not discuss it): for every i < n, the lists (dst[i], *, *) become what the lists (src[i], *, *) are -- prefix, window and its
+ * scores, so that decoding goes on from either, by itself, as it would have from the source.  What dst[i] held is released.
+ *   src, dst [n] int32, HOST (read before return): the slots of dst are distinct, and none of them is also in src; a
+ *            source may be given several times.  A source without a sequence makes one.
+ * Whole pages are not copied but shared: a full page is never written again.  Each child takes one page per list for the
+ * rows behind them (none if there are none) and copies the window.  A pool without a page left drops those rows
+ * and sets the status word to KVZAP_ERR_OOM_PAGES.  A step of beam search is one call, if beams that go on keep their slot.
+ */
+kvzap_status kvzap_cache_fork(kvzap_cache *cache, const int32_t *src, const int32_t *dst, int32_t n, void *stream);
+
+/*
+ * All lists of some sequences as dense rows, and back: to swap a sequence out of the cache, or to hand it to another
+ * process.  The lists of slots seqs[0 .. n) follow one another in the order (i, layer, head); list j = (i * L + layer) * H + head
+ * has rows row_start[j] .. row_start[j + 1] - 1: its prefix, then its window, oldest row first (as kvzap_cache_export).
+ *   seqs [n] int32, HOST (read before return): distinct slots; n <= 256 and n * L * H <= 24576 (else KVZAP_ERR_UNSUPPORTED)
+ *   K, V [capacity_rows, D] bf16;  row_start [n * L * H + 1] int64, from 0 on
+ *   n_tokens [n * L * H] int32: tokens appended so far; the list's last min(n_tokens, window) rows are its window
+ *   scores [n * L * H, window] fp32: the buffered scores of the window's tokens, oldest first; behind them zeros (out), unread (in)
+ * kvzap_cache_pack writes all of these (scores_out may be NULL); rows from capacity_rows on are not copied.
+ * kvzap_cache_unpack releases what the slots held and gives them the packed sequences, pages from the cache's allocator
+ * (scores are required if window > 0).  n_rows is the number of rows that K and V have: none behind it is read.  A list with fewer rows
+ * than its window should have has that many tokens.  A pool or page table that is too small drops rows from the end of the prefix and
+ * sets the status word to KVZAP_ERR_OOM_PAGES.  Unpacked into any slots of a cache of the same shape (pages may be of
+ * another size), the sequences go on as they would have in their own.
+ */
+kvzap_status kvzap_cache_pack(kvzap_cache *cache, const int32_t *seqs, int32_t n, void *K_out, void *V_out,
+                              int64_t capacity_rows, int64_t *row_start, int32_t *n_tokens, float *scores_out, void *stream);
+kvzap_status kvzap_cache_unpack(kvzap_cache *cache, const int32_t *seqs, int32_t n, const void *K, const void *V,
+                                int64_t n_rows, const int64_t *row_start, const int32_t *n_tokens, const float *scores,
+                                void *stream);
+
+/*
+ * Tells which sequences are to be read together by kvzap_decode_attention_shared: group g is slots
+ * seqs[group_start[g]] .. seqs[group_start[g + 1] - 1].  What the lists of a group have in common -- for every layer and head the
+ * leading whole pages that are the same in the page tables of all members that hold a sequence -- is found by this call, on the device, and
+ * stays so while they decode: pages are only added behind.  Call it again when sequences were forked, or joined a group.  A member that is
+ * released, forked into, unpacked into or imported over counts as alone from then on, the others go on sharing.
+ *   group_start [n_groups + 1], seqs int32, HOST (read before return); a slot is in one group at most, others are read by themselves
+ *   n_q_heads: query heads of the attention calls to come (1..8 times the KV heads)
+ * n_groups = 0 takes all groups back.  The first call allocates device memory (up to some 64 MB, or what one layer needs; more only
+ * for larger groups), a later one may.  Same limits on D, pages and window as kvzap_decode_attention.
+ */
+kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, const int32_t *seqs, int32_t n_groups,
+                               int32_t n_q_heads, void *stream);
+
+/*
+ * kvzap_decode_attention over a cache with groups (kvzap_cache_share): the same operation with the same arguments, but the rows
+ * that a group shares are read once for all its members.  Results differ from kvzap_decode_attention's by rounding only,
+ * whatever was released or forked since the groups were told.  Without groups it is that call.  Two launches (for many layers
+ * some pairs of them).  KVZAP_ERR_INVALID_ARG for another n_q_heads than the groups were told for.
+ * In a captured graph the groups are those of the capture; a replay after another kvzap_cache_share reads every list by itself.
+ */
+kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
+                                           const void *Q, int32_t n_q_heads, float scale, void *O, void *stream);
 
 /* lengths [n_seqs, L, H] int32 (device): rows currently held by each list (prefix + window). */
 kvzap_status kvzap_cache_lengths(kvzap_cache *cache, int32_t *lengths, void *stream);
@@ -527,7 +639,8 @@ kvzap_status kvzap_prefill_to_cache_batch(kvzap_ctx *ctx, kvzap_cache *cache, in
  * cache states): prefix_len [n_seqs*L*H] and page_table
  * [n_seqs*L*H, max_pages_per_list], device int32 in list order (seq, layer,
  * head); next_free_page is the first pool page the allocator may hand out.
- * Every list's window becomes empty.  Synchronises `stream`.
+ * Every list's window becomes empty.  A page may be in the tables of several lists if it is full in each (as
+ * kvzap_cache_fork leaves them).  Synchronises `stream`.
  */
 kvzap_status kvzap_cache_import(kvzap_cache *cache, const int32_t *prefix_len, const int32_t *page_table,
                                 int32_t next_free_page, void *stream);

@@ -38,6 +38,22 @@ class KvzapConfig(ctypes.Structure):
                 ("max_tokens", ctypes.c_int64), ("max_seqs", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
+class KvzapRotaryConfig(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_context", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+ROWS_ROTATE, ROWS_8BIT = 1, 2
+
+
+class KvzapRows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("in_token", ctypes.c_int64), ("in_head", ctypes.c_int64),
+                ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64), ("n_heads", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
+
+
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 
 # name -> (restype, argtypes); also the list of symbols the header declares
@@ -78,6 +94,13 @@ SIGNATURES = {
     "kvzap_decode_attention": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_decode_attention_fp8": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_cache_release_seq": (_i32, [_vp, _i32, _vp]),
+    "kvzap_cache_fork": (_i32, [_vp, _vp, _vp, _i32, _vp]),
+    "kvzap_cache_pack": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp]),
+    "kvzap_cache_unpack": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp]),
+    "kvzap_cache_share": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp]),
+    "kvzap_decode_attention_shared": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
+    "kvzap_set_rotary": (_i32, [_vp, ctypes.POINTER(KvzapRotaryConfig)]),
+    "kvzap_rotary": (_i32, [_vp, _vp, _i64, ctypes.POINTER(KvzapRows), _i32, _i32, _vp]),
     "kvzap_cache_lengths": (_i32, [_vp, _vp, _vp]),
     "kvzap_cache_export": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _vp]),
     "kvzap_prefill_to_cache": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _i64, _f32, _vp, _vp]),
@@ -366,6 +389,73 @@ def kvzap_decode_step_fp8(handle, cache, layer_begin, layer_end, hidden_e4m3, x_
 
 def kvzap_cache_release_seq(handle, cache, seq, stream=None):
     _check(handle, load().kvzap_cache_release_seq(cache, seq, _stream(stream)))
+
+
+def _ints(values):
+    return (ctypes.c_int32 * max(len(values), 1))(*values)
+
+
+def kvzap_cache_fork(handle, cache, src, dst, stream=None):
+    """src, dst: slot numbers (host)."""
+    if len(src) != len(dst):
+        raise ValueError("fork: %d sources and %d destinations" % (len(src), len(dst)))
+    _check(handle, load().kvzap_cache_fork(cache, _ints(src), _ints(dst), len(src), _stream(stream)))
+
+
+def kvzap_cache_pack(handle, cache, seqs, K_out, V_out, row_start, n_tokens, scores_out=None, stream=None):
+    _check(handle, load().kvzap_cache_pack(cache, _ints(seqs), len(seqs), _ptr(K_out), _ptr(V_out), K_out.shape[0], _ptr(row_start),
+                                           _ptr(n_tokens), _ptr(scores_out), _stream(stream)))
+
+
+def kvzap_cache_unpack(handle, cache, seqs, K, V, row_start, n_tokens, scores, stream=None):
+    _check(handle, load().kvzap_cache_unpack(cache, _ints(seqs), len(seqs), _ptr(K), _ptr(V), K.shape[0], _ptr(row_start),
+                                             _ptr(n_tokens), _ptr(scores), _stream(stream)))
+
+
+def kvzap_cache_share(handle, cache, groups, n_q_heads, stream=None):
+    """groups: lists of slot numbers (host)."""
+    start = [0]
+    for g in groups:
+        start.append(start[-1] + len(g))
+    _check(handle, load().kvzap_cache_share(cache, _ints(start), _ints([b for g in groups for b in g]), len(groups), n_q_heads,
+                                            _stream(stream)))
+
+
+def kvzap_decode_attention_shared(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None):
+    """Q, O [layer_end - layer_begin, n_seqs, n_q_heads, D] bf16 on the device."""
+    _check(handle, load().kvzap_decode_attention_shared(handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O),
+                                                        _stream(stream)))
+
+
+def kvzap_set_rotary(handle, head_dim, rotary_dim, base=10000.0, interleaved=False, factor=1.0, original_context=0.0, low=1.0,
+                     high=4.0, magnitude=1.0, inv_freq=None):
+    cfg = KvzapRotaryConfig(head_dim, rotary_dim, 1 if interleaved else 0, magnitude, base, factor, original_context, low, high)
+    if inv_freq is not None:
+        if len(inv_freq) != rotary_dim // 2:
+            raise ValueError("inv_freq has %d values, rotary_dim %d needs %d" % (len(inv_freq), rotary_dim, rotary_dim // 2))
+        keep = (ctypes.c_double * len(inv_freq))(*[float(f) for f in inv_freq])
+        cfg.inv_freq = ctypes.cast(keep, ctypes.POINTER(ctypes.c_double))
+    _check(handle, load().kvzap_set_rotary(handle, ctypes.byref(cfg)))
+
+
+def rotary_rows(x, out, rotate):
+    """One tensor of kvzap_rotary: x [T, heads, D] bf16 -> out [T, heads, D] bf16 or [T, heads, D + 16] uint8 (8-bit rows); views with any
+    strides whose last dimension is contiguous."""
+    rows8 = out.dtype == torch.uint8
+    want = x.shape[:2] + ((x.shape[2] + 16,) if rows8 else x.shape[2:])
+    if x.dim() != 3 or x.dtype != torch.bfloat16 or (not rows8 and out.dtype != torch.bfloat16) or tuple(out.shape) != tuple(want):
+        raise ValueError("rows must be bf16 [T, heads, D] -> bf16 of that shape or uint8 [T, heads, D + 16], got %s -> %s" % (
+            tuple(x.shape), tuple(out.shape)))
+    if not x.is_cuda or out.device != x.device or (x.numel() and (x.stride(2) != 1 or out.stride(2) != 1)):
+        raise ValueError("rows must lie on one CUDA device, their elements side by side")
+    return KvzapRows(x.data_ptr() if x.numel() else None, out.data_ptr() if x.numel() else None, x.stride(0), x.stride(1),
+                     out.stride(0), out.stride(1), x.shape[1], (ROWS_ROTATE if rotate else 0) | (ROWS_8BIT if rows8 else 0))
+
+
+def kvzap_rotary(handle, positions, rows, inverse=False, stream=None):
+    """rows: what rotary_rows() makes of up to three tensors of the same tokens."""
+    _check(handle, load().kvzap_rotary(handle, _ptr(positions), positions.shape[0], (KvzapRows * len(rows))(*rows), len(rows),
+                                       1 if inverse else 0, _stream(stream)))
 
 
 def kvzap_cache_lengths(handle, cache, lengths, stream=None):
@@ -680,6 +770,35 @@ class Kvzap:
                                  lengths, tau_out, stream)
         return K_out, V_out, lengths
 
+    def set_rotary(self, rotary_dim=None, head_dim=None, base=10000.0, interleaved=False, factor=1.0, original_context=0.0, low=1.0,
+                   high=4.0, magnitude=1.0, inv_freq=None):
+        """Frequencies of rotary() (see kvzap_rotary_config in the header); head_dim: elements per head, the context's by default."""
+        head_dim = self.head_dim if head_dim is None else head_dim
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        kvzap_set_rotary(self.handle, head_dim, rotary_dim, base, interleaved, factor, original_context, low, high, magnitude, inv_freq)
+        self._rotary_head_dim = head_dim
+
+    def rotary(self, positions, Q=None, K=None, V=None, Q_out=None, K_out=None, V_out=None, inverse=False, stream=None):
+        """Q and K [T, heads, D] (any strides, e.g. columns of a fused projection) with the positions of their tokens applied, V as it
+        is, in one launch.  Outputs: bf16 rows of the same shape (given, or new and contiguous; a transposed view of a [heads, T, D]
+        buffer gives the layout of the pruning calls), or uint8 [T, heads, D + 16] given for 8-bit rows.  Returns those of the given inputs."""
+        if positions.dim() != 1 or positions.dtype != torch.int32:
+            raise ValueError("positions must be int32 [T]")
+        rows, outs = [], []
+        for x, out, rotate in ((Q, Q_out, True), (K, K_out, True), (V, V_out, False)):
+            if x is None:
+                continue
+            if x.dim() != 3 or x.shape[0] != positions.shape[0] or x.shape[2] != getattr(self, "_rotary_head_dim", x.shape[2]):
+                raise ValueError("rows must be [%d, heads, %s], got %s" % (positions.shape[0], getattr(self, "_rotary_head_dim", "D"), tuple(x.shape)))
+            if out is None:
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            rows.append(rotary_rows(x, out, rotate))
+            outs.append(out)
+        if not rows:
+            raise ValueError("rotary: no tensor given")
+        kvzap_rotary(self.handle, positions, rows, inverse, stream)
+        return outs[0] if len(outs) == 1 else tuple(outs)
+
     def create_cache(self, n_seqs, window, page_tokens, K_pool, V_pool, max_pages_per_list) -> "KvzapCache":
         return KvzapCache(self, n_seqs, window, page_tokens, K_pool, V_pool, max_pages_per_list)
 
@@ -722,6 +841,63 @@ class KvzapCache:
             scale = 1.0 / float(self.ctx.head_dim) ** 0.5
         kvzap_decode_attention(self.ctx.handle, self.handle, layer_begin, layer_end, Q, scale, out, stream)
         return out
+
+    def share(self, groups, n_q_heads, stream=None):
+        """Lists of slots whose common leading pages attention_shared() reads once for all of them; [] takes all groups back."""
+        kvzap_cache_share(self.ctx.handle, self.handle, groups, n_q_heads, stream)
+
+    def attention_shared(self, layer_begin, layer_end, Q, scale=None, out=None, stream=None):
+        """attention() with the rows that the groups told by share() have in common read once for each group."""
+        if out is None:
+            out = torch.empty_like(Q)
+        if scale is None:
+            scale = 1.0 / float(self.ctx.head_dim) ** 0.5
+        kvzap_decode_attention_shared(self.ctx.handle, self.handle, layer_begin, layer_end, Q, scale, out, stream)
+        return out
+
+    def fork(self, src, dst, stream=None):
+        """The sequences of slots dst become copies of those of slots src (lists of the same length); whole pages are shared."""
+        kvzap_cache_fork(self.ctx.handle, self.handle, src, dst, stream)
+
+    def pack(self, seqs, K_out=None, V_out=None, row_start=None, n_tokens=None, scores_out=None, stream=None):
+        """All lists of some slots as dense rows -> (K, V [rows, D], row_start, n_tokens, scores), what unpack() takes.  Without K_out the
+        rows are counted first, which waits for the device."""
+        ctx = self.ctx
+        lists = len(seqs) * ctx.n_layers * ctx.n_kv_heads
+        if K_out is None:
+            stream_ = torch.cuda.current_stream() if stream is None else stream
+            with torch.cuda.stream(stream_):
+                rows = int(self.lengths(stream)[torch.tensor(seqs, device=ctx.device)].sum().item())
+            K_out = torch.empty(rows, ctx.head_dim, dtype=torch.bfloat16, device=ctx.device)
+        if V_out is None:
+            V_out = torch.empty_like(K_out)
+        if row_start is None:
+            row_start = torch.empty(lists + 1, dtype=torch.int64, device=ctx.device)
+        if n_tokens is None:
+            n_tokens = torch.empty(lists, dtype=torch.int32, device=ctx.device)
+        if scores_out is None:
+            scores_out = torch.empty(lists, self.window, dtype=torch.float32, device=ctx.device)
+        self._check_packed(len(seqs), K_out, V_out, row_start, n_tokens, scores_out)
+        kvzap_cache_pack(ctx.handle, self.handle, seqs, K_out, V_out, row_start, n_tokens, scores_out, stream)
+        return K_out, V_out, row_start, n_tokens, scores_out
+
+    def unpack(self, seqs, K, V, row_start, n_tokens, scores, stream=None):
+        """Gives the slots the sequences that pack() has written; what they held is released."""
+        self._check_packed(len(seqs), K, V, row_start, n_tokens, scores)
+        kvzap_cache_unpack(self.ctx.handle, self.handle, seqs, K, V, row_start, n_tokens, scores, stream)
+
+    def _check_packed(self, n, K, V, row_start, n_tokens, scores):
+        lists = n * self.ctx.n_layers * self.ctx.n_kv_heads
+        if K.dim() != 2 or K.shape[1] != self.ctx.head_dim or K.shape != V.shape or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16:
+            raise ValueError("K and V must be bf16 [rows, %d], got %s and %s" % (self.ctx.head_dim, tuple(K.shape), tuple(V.shape)))
+        if row_start.numel() != lists + 1 or row_start.dtype != torch.int64 or n_tokens.numel() != lists or n_tokens.dtype != torch.int32:
+            raise ValueError("row_start must be int64 [%d] and n_tokens int32 [%d]" % (lists + 1, lists))
+        if scores.numel() != lists * self.window or scores.dtype != torch.float32:
+            raise ValueError("scores must be fp32 [%d, %d]" % (lists, self.window))
+
+    def import_prefix(self, prefix_len, page_table, next_free_page, stream=None):
+        """Installs page tables made elsewhere (kvzap_cache_import): every list's prefix, all windows empty."""
+        kvzap_cache_import(self.ctx.handle, self.handle, prefix_len, page_table, next_free_page, stream)
 
     def release_seq(self, seq, stream=None):
         """The sequence in slot `seq` has ended: its lists become empty and its pages are handed out again."""

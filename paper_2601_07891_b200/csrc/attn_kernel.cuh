@@ -65,6 +65,7 @@
 
 #include "decode_kernels.cuh"
 #include "ptx.cuh"
+#include "shared_attn_kernel.cuh"
 
 namespace kvzap {
 
@@ -99,6 +100,7 @@ struct AttnParams {
     int32_t tiles_shift;        // logarithm of the tiles per page, or -1
     int32_t beside_ctas;        // kBeside: CTAs [0, beside_ctas) run beside the step, as many as find room
     int32_t beside_tiles;       // n_parts == 0: with more tiles than this in all lists all CTAs wait for the step
+    ShareView share;            // kShared: what shared_attn_kernel, ahead of this launch, leaves of the lists' shared rows
 };
 
 // The lists of a call, of lengths[0 .. n) tiles, cut into at most n_units (>= n) parts: a list of t tiles has
@@ -214,7 +216,10 @@ __device__ __forceinline__ void attn_store(uint16_t *out, const float4 &num, flo
 
 // kBeside: the launch may run beside the step ahead of it; a kernel of its own, since what that takes (the rest of a list learnt
 // late, queries read twice, more code) costs a launch 2 to 5 us where nothing runs beside it: behind other work of the caller.
-template <int kD, bool kFp8, bool kBeside>
+// kShared: the launch behind a shared_attn_kernel over the same layers, which takes the rows that the lists share with those of
+// their groups (share_rows, whole tiles at the lists' beginnings); this one takes the others, beside it as far as SMs are free (that launch
+// lets it start when everything ahead of it has completed), waits for it only at the end, and joins the two.
+template <int kD, bool kFp8, bool kBeside, bool kShared = false>
 __global__ void __launch_bounds__(kAttnThreads, kFp8 ? 4 : 3)
 decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_constant__ CUtensorMap tmap_vpool,
                    const __grid_constant__ CUtensorMap tmap_kring, const __grid_constant__ CUtensorMap tmap_vring,
@@ -260,7 +265,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     // How long the lists were before the step, by which the CTAs of a launch share them out, all read in c.before: it does
     // not change while this launch runs.  CTAs that find no room beside the step wait for it first.
     bool beside = kBeside && static_cast<int>(blockIdx.x) < p.beside_ctas;
-    if (!beside) griddep_wait();
+    if (!beside && !kShared) griddep_wait();
 
     int list, part, n_parts = p.n_parts;
     int32_t n_before = 0;                   // kBeside: prefix rows that nothing ahead of this launch still touches
@@ -269,6 +274,9 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     auto cache_list = [&](int i) {          // list i of the call among the cache's lists
         return (static_cast<int64_t>((i / H) % B) * c.n_layers + p.layer0 + i / (H * B)) * H + i % H;
     };
+    const bool grouped = kShared && __ldcg(p.share.stamp_now) == p.share.stamp;
+    auto shared_rows = [&](int i) { return kShared && grouped ? __ldcg(c.share_rows + cache_list(i)) : 0; };
+    int32_t n_shared = 0;                   // kShared: of this list
     if (n_parts > 0) {
         const int extra = static_cast<int>(blockIdx.x) - p.extra0;
         if (extra < 0) {
@@ -283,9 +291,10 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         if (!beside) {
             n_total = __ldcg(c.n_tokens + cache_list(list));
             n_prefix = __ldcg(c.prefix_len + cache_list(list));
+            n_shared = shared_rows(list);
         }
         if (list >= p.head_lists) {
-            const int tiles = ((kBeside ? n_before : n_prefix) + min(kBeside ? c.window : n_total, c.window)) / kAttnTileRows;
+            const int tiles = ((kBeside ? n_before : n_prefix) - n_shared + min(kBeside ? c.window : n_total, c.window)) / kAttnTileRows;
             // as many as the other lists have, or more; a list that is over in 16 tiles has one
             n_parts = tiles < 16 ? 1 : max(n_parts, min(p.tail_parts, tiles / kAttnTailTiles));
             if (part >= n_parts) {                                 // the whole CTA
@@ -302,7 +311,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             int2 n = make_int2(__ldcg(before + cache_list(i)), beside ? 0 : __ldcg(c.n_tokens + cache_list(i)));
             if (kBeside) n.x = min(n.x, __ldcg(c.prefix_len + cache_list(i)));      // it never is less, nor may it be
             counts[i] = n;
-            lengths[i] = (n.x + kAttnTileRows - 1) / kAttnTileRows + ((kBeside ? c.window : min(n.y, c.window)) + kAttnTileRows - 1) / kAttnTileRows;
+            lengths[i] = (n.x - shared_rows(i) + kAttnTileRows - 1) / kAttnTileRows + ((kBeside ? c.window : min(n.y, c.window)) + kAttnTileRows - 1) / kAttnTileRows;
         }
         __syncthreads();
         // One wave: beside the step, on the SMs that it leaves, if what that adds to the wave's time is less than the step's;
@@ -323,11 +332,12 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         }
         n_parts = attn_unit(lengths, n_lists, n_units, blockIdx.x, lane, list, part);
         if (n_parts == 0) {                                        // the whole CTA: more CTAs than parts
-            griddep_wait();
+            if (!kShared) griddep_wait();
             return;
         }
         n_before = n_prefix = counts[list].x;
         n_total = counts[list].y;
+        n_shared = shared_rows(list);
         if (kBeside && !beside) n_prefix = __ldcg(c.prefix_len + cache_list(list));
         fence_proxy_async_smem();                                  // the copies below write where these were read
         __syncthreads();
@@ -349,6 +359,11 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         t_first = static_cast<int>(static_cast<int64_t>(n_run) * part / n_parts);
         n_tiles = static_cast<int>(static_cast<int64_t>(n_run) * (part + 1) / n_parts);
         if (kBeside) n_early = n_tiles -= t_first;
+        if constexpr (kShared) {            // the same tiles without the first ones
+            const int skip = n_shared / kAttnTileRows, n_own = n_run - skip;
+            t_first = skip + static_cast<int>(static_cast<int64_t>(n_own) * part / n_parts);
+            n_tiles = skip + static_cast<int>(static_cast<int64_t>(n_own) * (part + 1) / n_parts);
+        }
     }
     const int s_first = kBeside ? 0 : t_first;
     // kBeside, per warp, in shared memory for want of registers: what the main loop seldom needs
@@ -806,6 +821,53 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     const int unit0 = p.n_parts == 0 ? static_cast<int>(blockIdx.x) - part
                       : list >= p.head_lists ? p.tail_unit0 + (list - p.head_lists) * p.tail_parts : list * p.n_parts;
     float *unit = n_parts > 1 ? p.part_scratch + static_cast<int64_t>(unit0 + part) * kUnit : nullptr;
+    // kShared: what shared_attn_kernel has left of the list's shared rows, added to four elements of one query head
+    const float *sh_part = nullptr;
+    const float2 *sh_ml = nullptr;
+    int64_t sh_stride = 0;
+    int sh_n = 0;
+    if constexpr (kShared) {
+        if (n_shared > 0) {
+            const int h = list % H, b = (list / H) % B, l = list / (H * B);
+            const int unit = (l * p.share.n_subs + __ldcg(p.share.seq_sub + b)) * H + h;
+            const int32_t *tile0 = p.share.tile0 + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
+            const int64_t base = __ldcg(tile0), tiles = __ldcg(tile0 + static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H) - base;
+            const int ctas = share_ctas(tiles, p.share.n_ctas);
+            const int c0 = share_owner(tiles, ctas, __ldcg(tile0 + unit) - base), c1 = share_owner(tiles, ctas, __ldcg(tile0 + unit + 1) - base - 1);
+            const int64_t row = static_cast<int64_t>(c0 + unit) * p.share.rows_max + __ldcg(p.share.seq_pos + b) * p.group;
+            sh_part = p.share.part + row * kD;
+            sh_ml = p.share.part_ml + row;
+            sh_stride = p.share.rows_max;
+            sh_n = c1 - c0 + 1;
+        }
+    }
+    auto join_shared = [&](int gq, int d, float &m_all, float &den, float4 &num) {
+        constexpr int kPieces = 4;
+        for (int i0 = 0; i0 < sh_n; i0 += kPieces) {
+            float2 ml[kPieces];
+            float4 nv[kPieces];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int64_t at = (i0 + j) * sh_stride + gq;
+                const bool in = i0 + j < sh_n;
+                ml[j] = in ? __ldcg(sh_ml + at) : make_float2(-INFINITY, 0.0f);
+                nv[j] = in ? __ldcg(reinterpret_cast<const float4 *>(sh_part + at * kD + d)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                if (ml[j].y < 0.0f) den = -INFINITY;                    // a wait ran out there: zeros
+                if (!(ml[j].x > -INFINITY)) continue;
+                const float m_new = fmaxf(m_all, ml[j].x), f = m_all > -INFINITY ? fast_ex2(m_all - m_new) : 0.0f, g2 = fast_ex2(ml[j].x - m_new);
+                num.x *= f; num.y *= f; num.z *= f; num.w *= f;
+                attn_add(num, nv[j], g2);
+                den = den * f + ml[j].y * g2;
+                m_all = m_new;
+            }
+        }
+    };
+    if constexpr (kShared) {
+        if (n_parts == 1) griddep_wait();
+    }
     // four elements of one query head per thread
     for (int idx = threadIdx.x; idx < p.group * (kD / 4); idx += kAttnThreads) {
         const int gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
@@ -825,6 +887,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             }
         }
         if (n_parts == 1) {
+            if constexpr (kShared) join_shared(gq, d, m_all, den, num);
             attn_store(p.out + (out_row0 + gq) * kD + d, num, failed ? 0.0f : den);      // an empty list gives zeros
         } else {
             __stcg(reinterpret_cast<float4 *>(unit + 16 + gq * kD + d), num);
@@ -842,6 +905,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     if (threadIdx.x == 0) last_s = arrive_last(p.part_arrive + (list - p.list0), static_cast<uint32_t>(n_parts));
     __syncthreads();
     if (!last_s) return;
+    if constexpr (kShared) griddep_wait();
     const float *units = p.part_scratch + static_cast<int64_t>(unit0) * kUnit;
     constexpr int kBatch = 8;               // parts whose values are loaded together: one round trip to memory
     for (int idx = threadIdx.x; idx < p.group * (kD / 4); idx += kAttnThreads) {
@@ -875,6 +939,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
                 den += dv[j] * f;
             }
         }
+        if constexpr (kShared) join_shared(gq, d, m_all, den, num);
         attn_store(p.out + (out_row0 + gq) * kD + d, num, den);
     }
 }

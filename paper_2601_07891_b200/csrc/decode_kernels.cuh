@@ -36,6 +36,8 @@ struct CacheView {
     uint8_t *active;          // [n_seqs]
     // prefix_len before the last one-launch step behind an attention, for the attention beside it (see decode_attn_kernel)
     int32_t *before;          // [n_lists]
+    int32_t *page_refs;       // [n_pages_pool] owners of a page beyond the first (see pages_kernels.cuh)
+    int32_t *share_rows;      // [n_lists] leading rows that are read with the list's group (see shared_attn_kernel.cuh), 0: none
 };
 
 // One more page for a list: a released one if the stack has any, else the next never-used page of the
@@ -208,28 +210,6 @@ decode_update_kernel(const CacheView c, int layer0, int n_layers_call, const flo
                 c.score_ring[li * c.window + slot] = __ldcg(scores + src_row);
             }
         }
-    }
-}
-
-// A sequence has ended: the pages of all its lists (L x H of them, one warp each) go onto the stack of
-// released pages and the lists become empty.  Runs alone on the stream (it is the one kernel that adds
-// to the stack).
-__global__ void __launch_bounds__(32)
-release_seq_kernel(const CacheView c, int32_t seq)
-{
-    griddep_wait();              // and lets nothing start before it is done
-    const int64_t li = static_cast<int64_t>(seq) * c.n_layers * c.n_heads + blockIdx.x;
-    const int lane = threadIdx.x;
-    const int32_t n_pages = (c.prefix_len[li] + c.page_tokens - 1) / c.page_tokens;
-    int32_t base = 0;
-    if (lane == 0 && n_pages > 0) base = atomicAdd(c.free_top, n_pages);
-    base = __shfl_sync(0xffffffffu, base, 0);
-    for (int32_t i = lane; i < n_pages; i += 32) c.free_stack[base + i] = c.page_table[li * c.max_pages + i];
-    __syncwarp();
-    if (lane == 0) {
-        c.prefix_len[li] = 0;
-        c.n_tokens[li] = 0;
-        if (blockIdx.x == 0) c.active[seq] = 0;
     }
 }
 

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -18,8 +19,10 @@
 #include "attn_kernel.cuh"
 #include "inflight.h"
 #include "decode_kernels.cuh"
+#include "pages_kernels.cuh"
 #include "prune_kernels.cuh"
 #include "prune_onepass_kernel.cuh"
+#include "rotary_kernel.cuh"
 #include "score_kernel.cuh"
 #include "chunk_kernel.cuh"
 #include "score_linear_split_kernel.cuh"
@@ -178,6 +181,9 @@ struct kvzap_ctx {
     // another one is started without a wait only directly behind them, and if it conflicts with none of it; the scoring kernels
     // consult the list before they write a scores buffer early.
     kvzap::InFlight in_flight;
+    // positions (kvzap_set_rotary)
+    kvzap_rotary_config rotary;
+    std::vector<uint64_t> rotary_step;   // [rotary_dim / 2] turns a token in units of 2^-64; empty: not set
     static_assert(kvzap::InFlight::kMaxChain + 2 <= kvzap::kOpRing, "launches that run beside one another use scratch sets of their own");
     char err[512] = "";
 };
@@ -2233,6 +2239,148 @@ kvzap_status kvzap_set_wait_limit(kvzap_ctx *ctx, int64_t cycles)
     return KVZAP_OK;
 }
 
+kvzap_status kvzap_set_rotary(kvzap_ctx *ctx, const kvzap_rotary_config *cfg)
+{
+    if (!ctx || !cfg) return KVZAP_ERR_INVALID_ARG;
+    const int D = cfg->head_dim, R = cfg->rotary_dim;
+    if (D < 8 || D > 1024 || D % 8 != 0) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: head_dim %d is not a multiple of 8 in 8..1024", D);
+    if (R < 2 || R > D || R % 2 != 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: rotary_dim %d is not even, or outside 2..head_dim", R);
+    if (cfg->interleaved != 0 && cfg->interleaved != 1) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: interleaved is 0 or 1");
+    // NaN fails each of these
+    if (!cfg->inv_freq && !(cfg->base > 1.0 && cfg->base < 1e300)) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: base must be above 1");
+    if (!(cfg->factor >= 1.0 && cfg->factor < 1e9)) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: factor must be at least 1");
+    if (!(cfg->original_context >= 0.0 && cfg->original_context < 1e15)) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: original_context must be at least 0");
+    if (cfg->original_context > 0.0 && !(cfg->low >= 0.0 && cfg->high > cfg->low && cfg->high < 1e15))
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: 0 <= low < high is required");
+    if (!(cfg->magnitude > 0.0f && cfg->magnitude < 1e30f)) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: magnitude must be above 0");
+    std::vector<uint64_t> step;
+    try { step.resize(static_cast<size_t>(R / 2)); } catch (...) { return fail(ctx, KVZAP_ERR_CUDA, "out of host memory"); }
+    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    for (int i = 0; i < R / 2; ++i) {
+        double f = cfg->inv_freq ? cfg->inv_freq[i] : pow(cfg->base, -2.0 * i / R);
+        if (!(f >= 0.0 && f < 1e9)) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: frequency %d is not in 0..1e9", i);
+        double keep = 0.0;                                     // linear: all frequencies alike
+        if (cfg->original_context > 0.0) {
+            const double turns = cfg->original_context * f / kTwoPi;
+            keep = std::min(1.0, std::max(0.0, (turns - cfg->low) / (cfg->high - cfg->low)));
+        }
+        f *= keep + (1.0 - keep) / cfg->factor;
+        double whole;
+        const double part = modf(f / kTwoPi, &whole);          // whole turns a token are no turn
+        step[i] = static_cast<uint64_t>(ldexp(part, 64));      // part < 1 is at most 1 - 2^-53
+    }
+    ctx->rotary = *cfg;
+    ctx->rotary.inv_freq = nullptr;
+    ctx->rotary_step.swap(step);
+    return KVZAP_OK;
+}
+
+}  // extern "C"
+
+namespace kvzap {
+
+template <int kPairs>
+static kvzap_status launch_rotary(kvzap_ctx *ctx, const int32_t *positions, int64_t n_tokens, const kvzap_rows *tensors, int n_tensors,
+                                  bool inverse, bool fast, cudaStream_t stream)
+{
+    RotaryParams<kPairs> p;
+    memset(&p, 0, sizeof p);
+    const kvzap_rotary_config &r = ctx->rotary;
+    p.positions = positions;
+    p.n_tokens = n_tokens;
+    p.head_dim = r.head_dim;
+    p.rotary_dim = r.rotary_dim;
+    p.magnitude = r.magnitude;
+    p.sign = inverse ? -1.0f : 1.0f;
+    for (int i = 0; i < n_tensors; ++i) {
+        const kvzap_rows &t = tensors[i];
+        if (t.n_heads == 0) continue;
+        RotaryTensor &o = p.t[p.n_tensors++];
+        const bool rows8 = (t.flags & KVZAP_ROWS_8BIT) != 0;
+        o.in = static_cast<const uint8_t *>(t.in);
+        o.out = static_cast<uint8_t *>(t.out);
+        o.in_token = t.in_token * 2;
+        o.in_head = t.in_head * 2;
+        o.out_token = t.out_token * (rows8 ? 1 : 2);
+        o.out_head = t.out_head * (rows8 ? 1 : 2);
+        o.n_heads = t.n_heads;
+        o.flags = ((t.flags & KVZAP_ROWS_ROTATE) ? kRotRotate : 0u) | (rows8 ? kRotRows8 : 0u);
+        p.n_heads += t.n_heads;
+    }
+    for (size_t i = 0; i < ctx->rotary_step.size(); ++i) p.step[i] = ctx->rotary_step[i];
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    if (fast) {
+        // Heads at a time: all of a token's, as long as that makes no more threads than the device holds (few tokens: the shortest way
+        // through); else a warp per token, which works its sines out once for a dozen heads.
+        p.lanes = p.head_dim / 16;
+        p.rows = p.n_heads;
+        const int few = std::max(1, 32 / p.lanes);
+        if (n_tokens * p.lanes * p.n_heads > static_cast<int64_t>(ctx->sm_count) * 2048 && few < p.rows) p.rows = few;
+        const int64_t threads = n_tokens * p.lanes * p.rows, blocks = (threads + kRotThreads - 1) / kRotThreads;
+        if (blocks > 0x7fffffffLL) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: too many tokens for one launch");
+        make_launch(&cfg, attrs, dim3(static_cast<unsigned>(blocks)), dim3(kRotThreads), 0, stream, !ctx->profiling, 1);
+        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, r.interleaved ? rotary_kernel<kPairs, true> : rotary_kernel<kPairs, false>, p));
+    } else {
+        const int64_t items = n_tokens * (p.head_dim - p.rotary_dim / 2), blocks = (items + kRotThreads - 1) / kRotThreads;
+        make_launch(&cfg, attrs, dim3(static_cast<unsigned>(std::min<int64_t>(blocks, ctx->sm_count * 32))), dim3(kRotThreads), 0, stream,
+                    !ctx->profiling, 1);
+        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, r.interleaved ? rotary_odd_kernel<kPairs, true> : rotary_odd_kernel<kPairs, false>, p));
+    }
+    ctx->launches += 1;
+    return KVZAP_OK;
+}
+
+}  // namespace kvzap
+
+extern "C" {
+
+kvzap_status kvzap_rotary(kvzap_ctx *ctx, const int32_t *positions, int64_t n_tokens, const kvzap_rows *tensors, int32_t n_tensors,
+                          int32_t inverse, void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_rotary");
+    if (!ctx) return KVZAP_ERR_INVALID_ARG;
+    begin_op(ctx);
+    if (ctx->rotary_step.empty()) return fail(ctx, KVZAP_ERR_STATE, "rotary: the context has no frequencies (kvzap_set_rotary)");
+    if (n_tokens < 0 || !tensors || n_tensors < 1 || n_tensors > kRotTensors)
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: n_tokens >= 0 and 1..%d tensors are required", kRotTensors);
+    const int D = ctx->rotary.head_dim, R = ctx->rotary.rotary_dim;
+    bool fast = D % 16 == 0 && R % 16 == 0 && D <= 512, any = false;
+    int64_t heads = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const kvzap_rows &t = tensors[i];
+        const bool rows8 = (t.flags & KVZAP_ROWS_8BIT) != 0;
+        if (t.n_heads < 0 || t.n_heads > 65536 || (t.flags & ~(KVZAP_ROWS_ROTATE | KVZAP_ROWS_8BIT)) != 0)
+            return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: tensor %d: 0..65536 heads and KVZAP_ROWS_* flags are required", i);
+        if (rows8 && D != 64 && D != 128) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: 8-bit rows have 64 or 128 elements");
+        if (n_tokens == 0 || t.n_heads == 0) continue;
+        if (!t.in || !t.out) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: tensor %d is NULL", i);
+        const int64_t row = rows8 ? D + kAttnTrailerBytes : D;
+        if (t.in_token < 0 || t.in_head < 0 || t.out_token < 0 || t.out_head < 0 || (t.n_heads > 1 && t.out_head < row) ||
+            (n_tokens > 1 && t.out_token < row))
+            return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: tensor %d: strides must not be negative, and output rows not overlap", i);
+        if (t.in == t.out && (rows8 || t.in_token != t.out_token || t.in_head != t.out_head))
+            return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: tensor %d: in place, rows stay where they are", i);
+        if (reinterpret_cast<uintptr_t>(t.in) % 2 != 0 || reinterpret_cast<uintptr_t>(t.out) % (rows8 ? 16 : 2) != 0 ||
+            (rows8 && (t.out_token % 16 != 0 || t.out_head % 16 != 0)))
+            return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: tensor %d is not aligned (8-bit rows: 16 bytes)", i);
+        const bool al = aligned16(t.in) && aligned16(t.out) && t.in_token % 8 == 0 && t.in_head % 8 == 0 &&
+                        (rows8 || (t.out_token % 8 == 0 && t.out_head % 8 == 0));
+        if (rows8 && (!al || R % 16 != 0))
+            return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: tensor %d: 8-bit rows are made of 16-byte aligned ones, rotary_dim a multiple of 16", i);
+        fast = fast && al;
+        any = any || rows8;
+        heads += t.n_heads;
+    }
+    if (n_tokens == 0 || heads == 0) return KVZAP_OK;
+    if (!positions) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: positions are required");
+    if (any && !fast) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: beside 8-bit rows the other tensors are 16-byte aligned too");
+    DeviceGuard guard(ctx->cfg.device);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return R <= 128 ? launch_rotary<64>(ctx, positions, n_tokens, tensors, n_tensors, inverse != 0, fast, stream)
+                    : launch_rotary<512>(ctx, positions, n_tokens, tensors, n_tensors, inverse != 0, fast, stream);
+}
+
 kvzap_status kvzap_set_profiling(kvzap_ctx *ctx, int32_t enable)
 {
     if (!ctx) return KVZAP_ERR_INVALID_ARG;
@@ -2384,6 +2532,16 @@ struct kvzap_cache {
     float *attn_scratch = nullptr;       // partial results of lists that are split over several CTAs
     uint32_t *attn_arrive = nullptr;     // [attn_split_lists] arrival counts, zero between launches
     int64_t attn_units = 0;              // capacity of attn_scratch in (list, part) units
+    std::vector<char> empty;             // [n_seqs] slots that were released and have not been given anything since
+    // groups whose shared rows are read together (kvzap_cache_share); host view, then device buffers
+    int32_t share_subs = 0, share_q_heads = 0, share_rows_max = 0, share_stamp = 0;
+    int32_t share_box = 0;               // rows per copy of tm_kshare, tm_vshare; 0: not built
+    CUtensorMap tm_kshare, tm_vshare;
+    int32_t *share_meta = nullptr;       // [1] stamp, [n_seqs + 1] starts, [n_seqs] members, [n_seqs] group, [n_seqs] place there
+    int32_t *share_tile0 = nullptr;      // [L * n_seqs * H + 1]
+    void *share_part = nullptr;          // slots of (m, l), then of outputs
+    size_t share_part_bytes = 0;
+    int32_t share_layers = 0;            // layers of a launch, as far as the slots go
 };
 
 namespace kvzap {
@@ -2602,6 +2760,7 @@ kvzap_status kvzap_cache_create(kvzap_ctx *ctx, kvzap_cache **out, int32_t n_seq
     if (!cache) return fail(ctx, KVZAP_ERR_CUDA, "out of host memory");
     cache->ctx = ctx;
     cache->n_lists = static_cast<int64_t>(n_seqs) * c.n_layers * c.n_kv_heads;
+    try { cache->empty.assign(static_cast<size_t>(n_seqs), 0); } catch (...) { delete cache; return fail(ctx, KVZAP_ERR_CUDA, "out of host memory"); }
     CacheView &v = cache->v;
     memset(&v, 0, sizeof v);
     v.n_seqs = n_seqs; v.n_layers = c.n_layers; v.n_heads = c.n_kv_heads; v.row_units = c.head_dim / 8;
@@ -2622,6 +2781,8 @@ kvzap_status kvzap_cache_create(kvzap_ctx *ctx, kvzap_cache **out, int32_t n_seq
     alloc(reinterpret_cast<void **>(&v.prefix_len), sizeof(int32_t) * n, true);
     alloc(reinterpret_cast<void **>(&v.page_table), sizeof(int32_t) * n * max_pages_per_list, true);
     alloc(reinterpret_cast<void **>(&v.before), sizeof(int32_t) * n, false);
+    alloc(reinterpret_cast<void **>(&v.page_refs), sizeof(int32_t) * static_cast<size_t>(n_pages_pool > 0 ? n_pages_pool : 1), true);
+    alloc(reinterpret_cast<void **>(&v.share_rows), sizeof(int32_t) * n, true);
     alloc(reinterpret_cast<void **>(&v.page_cursor), sizeof(int32_t), true);
     alloc(reinterpret_cast<void **>(&v.free_stack), sizeof(int32_t) * static_cast<size_t>(n_pages_pool > 0 ? n_pages_pool : 1), false);
     alloc(reinterpret_cast<void **>(&v.free_top), sizeof(int32_t), true);
@@ -2684,7 +2845,8 @@ kvzap_status kvzap_cache_destroy(kvzap_cache *cache)
     cudaFree(cache->v.n_tokens); cudaFree(cache->v.prefix_len); cudaFree(cache->v.page_table);
     cudaFree(cache->v.page_cursor); cudaFree(cache->scores); cudaFree(cache->done);
     cudaFree(cache->v.free_stack); cudaFree(cache->v.free_top); cudaFree(cache->v.active);
-    cudaFree(cache->v.before);
+    cudaFree(cache->v.before); cudaFree(cache->v.page_refs); cudaFree(cache->v.share_rows);
+    cudaFree(cache->share_meta); cudaFree(cache->share_tile0); cudaFree(cache->share_part);
     cudaFree(cache->attn_scratch); cudaFree(cache->attn_arrive);
     delete cache;
     return KVZAP_OK;
@@ -2796,13 +2958,20 @@ static decltype(&decode_attn_kernel<128, false, false>) attn_kernel(int d_attn, 
                : (beside ? decode_attn_kernel<64, false, true> : decode_attn_kernel<64, false, false>);
 }
 
-static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
-                                   const void *Q, int32_t n_q_heads, float scale, void *O, void *stream_, bool fp8)
+static decltype(&decode_attn_kernel<128, false, false>) attn_shared_kernel(int d_attn)
 {
-    NvtxRange nvtx_range(fp8 ? "kvzap_decode_attention_fp8" : "kvzap_decode_attention");
-    if (!ctx || !cache || cache->ctx != ctx) return KVZAP_ERR_INVALID_ARG;
-    begin_op(ctx);
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    return d_attn == 128 ? decode_attn_kernel<128, false, false, true> : decode_attn_kernel<64, false, false, true>;
+}
+
+static decltype(&shared_attn_kernel<128>) shared_kernel(int head_dim)
+{
+    return head_dim == 128 ? shared_attn_kernel<128> : shared_attn_kernel<64>;
+}
+
+// The checks of an attention call, and what its first one builds.
+static kvzap_status attention_check(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
+                                    const void *Q, int32_t n_q_heads, float scale, void *O, bool fp8)
+{
     const kvzap_config &c = ctx->cfg;
     const CacheView &v = cache->v;
     if (layer_begin < 0 || layer_end > c.n_layers || layer_begin >= layer_end)
@@ -2813,7 +2982,6 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "attention: n_q_heads must be 1..%d times the number of KV heads",
                     kAttnMaxGroup);
     if (!(scale == scale) || scale < 0.0f) return fail(ctx, KVZAP_ERR_INVALID_ARG, "attention: scale must be >= 0");
-    DeviceGuard guard(c.device);
     // elements per row as the attention sees them: head_dim bf16 values, or head_dim * 2 - 16 E4M3 codes
     const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
     if (d_attn != 64 && d_attn != 128)
@@ -2847,6 +3015,7 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
                 cudaError_t e = cudaSuccess;
                 for (int beside = 0; beside < 2 && e == cudaSuccess; ++beside)
                     e = cudaFuncSetAttribute(attn_kernel(d_attn, fp8, beside != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+                if (!fp8 && e == cudaSuccess) e = cudaFuncSetAttribute(attn_shared_kernel(d_attn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
                 if (e == cudaSuccess) cache->attn_state = fp8 ? 2 : 1;
             }
         }
@@ -2857,6 +3026,25 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
                           "window multiples of %d, fewer than 2^31 rows, and a cache not yet used by kvzap_decode_attention"
                         : "attention needs head_dim 64 or 128, page_tokens and window multiples of %d, fewer than 2^31 rows",
                     kAttnTileRows);
+    return KVZAP_OK;
+}
+
+// share: behind a shared_attn_kernel over the same layers, whose results it joins; else nullptr
+static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
+                                   const void *Q, int32_t n_q_heads, float scale, void *O, void *stream_, bool fp8,
+                                   const ShareView *share = nullptr)
+{
+    NvtxRange nvtx_range(fp8 ? "kvzap_decode_attention_fp8" : "kvzap_decode_attention");
+    if (!ctx || !cache || cache->ctx != ctx) return KVZAP_ERR_INVALID_ARG;
+    begin_op(ctx);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const kvzap_config &c = ctx->cfg;
+    const CacheView &v = cache->v;
+    DeviceGuard guard(c.device);
+    const kvzap_status checked = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, fp8);
+    if (checked != KVZAP_OK) return checked;
+    // elements per row as the attention sees them: head_dim bf16 values, or head_dim * 2 - 16 E4M3 codes
+    const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
     AttnParams p;
     memset(&p, 0, sizeof p);
     p.c = v;
@@ -2886,7 +3074,7 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
     // layer, step and attention, us a layer: 8 sequences x 2176 rows a list 34.1 -> 24.2, 128 x 4736 rows 378 -> 357, 64 x 1664
     // 8-bit rows 79.8 -> 78.6.
     const unsigned long long capture = capture_of(stream);
-    if (ctx->trusted && !ctx->profiling && ctx->fused_capture == capture && ctx->fused_cache == cache && ctx->fused_seq + 1 == ctx->op_seq && ctx->fused_behind_attention &&
+    if (!share && ctx->trusted && !ctx->profiling && ctx->fused_capture == capture && ctx->fused_cache == cache && ctx->fused_seq + 1 == ctx->op_seq && ctx->fused_behind_attention &&
         ctx->fused_stream == stream && ctx->fused_layer0 <= layer_begin && layer_end <= ctx->fused_layer1 &&
         beside_pays(ctx, n_lists_call, per_sm, ctx->fused_ctas)) {
         beside = true;
@@ -2932,17 +3120,19 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
         if (v.page_tokens / kAttnTileRows == 1 << i) p.tiles_shift = i;
     p.part_scratch = cache->attn_scratch;
     p.part_arrive = cache->attn_arrive;
+    if (share) p.share = *share;
     {
         ProfScope prof(ctx, KVZAP_KERNEL_ATTENTION, stream);
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attrs[2];
         make_launch(&cfg, attrs, dim3(static_cast<unsigned>(n_ctas)), dim3(kAttnThreads), attn_smem_bytes(d_attn, fp8), stream,
                     !ctx->profiling, 1);
-        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_kernel(d_attn, fp8, beside), cache->tm_kpool, cache->tm_vpool, cache->tm_kring,
+        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share ? attn_shared_kernel(d_attn) : attn_kernel(d_attn, fp8, beside), cache->tm_kpool, cache->tm_vpool, cache->tm_kring,
                                            cache->tm_vring, p));
     }
     ctx->launches += 1;
     ctx->beside += beside ? 1 : 0;
+    if (share) return KVZAP_OK;
     // only now: a step may start beside this attention only if it is there
     ctx->attn_seq = ctx->op_seq;
     ctx->attn_stream = stream;
@@ -2965,6 +3155,52 @@ kvzap_status kvzap_decode_attention_fp8(kvzap_ctx *ctx, kvzap_cache *cache, int3
     return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, true);
 }
 
+}  // extern "C"
+
+namespace kvzap {
+
+// Releases slots (up to kSlotBatch of them); those that hold nothing are left out.
+static kvzap_status release_slots(kvzap_cache *cache, const int32_t *slots, int n, cudaStream_t stream)
+{
+    kvzap_ctx *ctx = cache->ctx;
+    SlotList list;
+    int m = 0;
+    for (int i = 0; i < n; ++i)
+        if (!cache->empty[slots[i]]) list.slot[m++] = slots[i];
+    if (m == 0) return KVZAP_OK;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    make_launch(&cfg, attrs, dim3(static_cast<unsigned>(cache->v.n_layers * cache->v.n_heads), static_cast<unsigned>(m)), dim3(32), 0,
+                stream, !ctx->profiling, 1);
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, release_seqs_kernel, cache->v, list));
+    ctx->launches += 1;
+    for (int i = 0; i < m; ++i) cache->empty[list.slot[i]] = 1;
+    return KVZAP_OK;
+}
+
+// Slots in range; with `distinct`, none of them twice.
+static kvzap_status check_slots(kvzap_cache *cache, const char *call, const int32_t *slots, int32_t n, bool distinct)
+{
+    kvzap_ctx *ctx = cache->ctx;
+    for (int i = 0; i < n; ++i)
+        if (slots[i] < 0 || slots[i] >= cache->v.n_seqs)
+            return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: sequence slot %d out of range", call, slots[i]);
+    if (!distinct) return KVZAP_OK;
+    try {
+        std::vector<int32_t> sorted(slots, slots + n);
+        std::sort(sorted.begin(), sorted.end());
+        for (int i = 1; i < n; ++i)
+            if (sorted[i] == sorted[i - 1]) return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: sequence slot %d given twice", call, sorted[i]);
+    } catch (...) {
+        return fail(ctx, KVZAP_ERR_CUDA, "out of host memory");
+    }
+    return KVZAP_OK;
+}
+
+}  // namespace kvzap
+
+extern "C" {
+
 kvzap_status kvzap_cache_release_seq(kvzap_cache *cache, int32_t seq, void *stream_)
 {
     if (!cache) return KVZAP_ERR_INVALID_ARG;
@@ -2972,12 +3208,318 @@ kvzap_status kvzap_cache_release_seq(kvzap_cache *cache, int32_t seq, void *stre
     begin_op(ctx);
     if (seq < 0 || seq >= cache->v.n_seqs) return fail(ctx, KVZAP_ERR_INVALID_ARG, "release: seq %d out of range", seq);
     DeviceGuard guard(ctx->cfg.device);
+    cache->empty[seq] = 0;                              // a slot that is empty already costs a launch here, as ever
+    return release_slots(cache, &seq, 1, static_cast<cudaStream_t>(stream_));
+}
+
+kvzap_status kvzap_cache_fork(kvzap_cache *cache, const int32_t *src, const int32_t *dst, int32_t n, void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_cache_fork");
+    if (!cache) return KVZAP_ERR_INVALID_ARG;
+    kvzap_ctx *ctx = cache->ctx;
+    begin_op(ctx);
+    if (n < 0 || (n > 0 && (!src || !dst))) return fail(ctx, KVZAP_ERR_INVALID_ARG, "fork: src and dst (host), n >= 0 are required");
+    kvzap_status st = check_slots(cache, "fork", src, n, false);
+    if (st == KVZAP_OK) st = check_slots(cache, "fork", dst, n, true);
+    if (st != KVZAP_OK) return st;
+    if (static_cast<int64_t>(cache->v.n_layers) * cache->v.n_heads > 65535)
+        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "fork: more than 65535 lists a sequence");
+    std::vector<int32_t> order, uses;
+    try {
+        std::vector<char> to(static_cast<size_t>(cache->v.n_seqs), 0);
+        for (int i = 0; i < n; ++i) to[dst[i]] = 1;
+        for (int i = 0; i < n; ++i)
+            if (to[src[i]])
+                return fail(ctx, KVZAP_ERR_INVALID_ARG, "fork: slot %d is both a source and a destination", src[i]);
+        order.resize(static_cast<size_t>(n));
+        uses.assign(static_cast<size_t>(cache->v.n_seqs), 0);
+    } catch (...) {
+        return fail(ctx, KVZAP_ERR_CUDA, "out of host memory");
+    }
+    DeviceGuard guard(ctx->cfg.device);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    // all releases first: a kernel that hands pages back does not run beside one that takes them
+    for (int i = 0; i < n; i += kSlotBatch) {
+        st = release_slots(cache, dst + i, std::min(n - i, kSlotBatch), stream);
+        if (st != KVZAP_OK) return st;
+    }
+    for (int i = 0; i < n; ++i) order[i] = i;
+    std::sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return src[a] != src[b] ? src[a] < src[b] : a < b; });
+    for (int i0 = 0; i0 < n; i0 += kSlotBatch) {
+        const int m = std::min(n - i0, kSlotBatch);
+        SlotPairs pairs;
+        for (int i = 0; i < m; ++i) {
+            pairs.src[i] = src[order[i0 + i]];
+            pairs.dst[i] = dst[order[i0 + i]];
+            pairs.first[i] = 0;
+            uses[pairs.src[i]] += 1;
+        }
+        for (int i = 0; i < m; ++i) { pairs.first[i] = uses[pairs.src[i]]; uses[pairs.src[i]] = 0; }
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attrs[2];
+        make_launch(&cfg, attrs, dim3(static_cast<unsigned>(m), static_cast<unsigned>(cache->v.n_layers * cache->v.n_heads)), dim3(kForkThreads),
+                    0, stream, !ctx->profiling, 1);
+        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, fork_kernel, cache->v, pairs, ctx->status_dev));
+        ctx->launches += 1;
+        for (int i = 0; i < m; ++i) cache->empty[pairs.dst[i]] = cache->empty[pairs.src[i]];
+    }
+    return KVZAP_OK;
+}
+
+}  // extern "C"
+
+namespace kvzap {
+
+template <bool kOut>
+static kvzap_status launch_pack(kvzap_cache *cache, const PackArgs &a, const SlotList &list, cudaStream_t stream)
+{
+    kvzap_ctx *ctx = cache->ctx;
+    const size_t smem = sizeof(int64_t) * (static_cast<size_t>(a.n_lists) + 1);
+    KVZAP_CUDA(ctx, cudaFuncSetAttribute(pack_kernel<kOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(int64_t) * (kPackLists + 1))));
+    const int per_sm = smem <= 24 * 1024 ? 8 : smem <= 96 * 1024 ? 2 : 1;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attrs[2];
-    make_launch(&cfg, attrs, dim3(static_cast<unsigned>(cache->v.n_layers * cache->v.n_heads)), dim3(32), 0,
-                static_cast<cudaStream_t>(stream_), !ctx->profiling, 1);
-    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, release_seq_kernel, cache->v, seq));
+    make_launch(&cfg, attrs, dim3(static_cast<unsigned>(ctx->sm_count * per_sm)), dim3(kPackThreads), smem, stream, !ctx->profiling, 1);
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, pack_kernel<kOut>, a, list));
     ctx->launches += 1;
+    return KVZAP_OK;
+}
+
+static kvzap_status pack_args(kvzap_cache *cache, const char *call, PackArgs *a, SlotList *list, const int32_t *seqs, int32_t n,
+                              const void *K, const void *V, int64_t capacity_rows, const int64_t *row_start, const int32_t *n_tokens,
+                              const float *scores)
+{
+    kvzap_ctx *ctx = cache->ctx;
+    const CacheView &v = cache->v;
+    if (n < 1 || !seqs || !row_start || !n_tokens || capacity_rows < 0 || (capacity_rows > 0 && (!K || !V)) || !aligned16(K) || !aligned16(V))
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: seqs (host), n >= 1, row_start, n_tokens and 16-byte aligned K and V are required", call);
+    const int64_t n_lists = static_cast<int64_t>(n) * v.n_layers * v.n_heads;
+    if (n > kSlotBatch || n_lists > kPackLists)
+        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "%s: more than %d sequences or %d lists in one call", call, kSlotBatch, kPackLists);
+    kvzap_status st = check_slots(cache, call, seqs, n, true);
+    if (st != KVZAP_OK) return st;
+    memset(a, 0, sizeof *a);
+    a->c = v;
+    a->K = static_cast<uint4 *>(const_cast<void *>(K));
+    a->V = static_cast<uint4 *>(const_cast<void *>(V));
+    a->capacity_rows = capacity_rows;
+    a->row_start = const_cast<int64_t *>(row_start);
+    a->n_tokens = const_cast<int32_t *>(n_tokens);
+    a->scores = const_cast<float *>(scores);
+    a->n_lists = static_cast<int32_t>(n_lists);
+    a->status = ctx->status_dev;
+    for (int i = 0; i < n; ++i) list->slot[i] = seqs[i];
+    return KVZAP_OK;
+}
+
+}  // namespace kvzap
+
+extern "C" {
+
+kvzap_status kvzap_cache_pack(kvzap_cache *cache, const int32_t *seqs, int32_t n, void *K_out, void *V_out, int64_t capacity_rows,
+                              int64_t *row_start, int32_t *n_tokens, float *scores_out, void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_cache_pack");
+    if (!cache) return KVZAP_ERR_INVALID_ARG;
+    begin_op(cache->ctx);
+    PackArgs a;
+    SlotList list;
+    kvzap_status st = pack_args(cache, "pack", &a, &list, seqs, n, K_out, V_out, capacity_rows, row_start, n_tokens, scores_out);
+    if (st != KVZAP_OK) return st;
+    DeviceGuard guard(cache->ctx->cfg.device);
+    return launch_pack<true>(cache, a, list, static_cast<cudaStream_t>(stream_));
+}
+
+kvzap_status kvzap_cache_unpack(kvzap_cache *cache, const int32_t *seqs, int32_t n, const void *K, const void *V, int64_t n_rows,
+                                const int64_t *row_start, const int32_t *n_tokens, const float *scores, void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_cache_unpack");
+    if (!cache) return KVZAP_ERR_INVALID_ARG;
+    kvzap_ctx *ctx = cache->ctx;
+    begin_op(ctx);
+    PackArgs a;
+    SlotList list;
+    kvzap_status st = pack_args(cache, "unpack", &a, &list, seqs, n, K, V, n_rows, row_start, n_tokens, scores);
+    if (st != KVZAP_OK) return st;
+    if (!scores && cache->v.window > 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "unpack: the scores of the windows' tokens are required");
+    DeviceGuard guard(ctx->cfg.device);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    st = release_slots(cache, seqs, n, stream);
+    if (st != KVZAP_OK) return st;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    make_launch(&cfg, attrs, dim3(static_cast<unsigned>(a.n_lists)), dim3(32), 0, stream, !ctx->profiling, 1);
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, unpack_pages_kernel, a, list));
+    ctx->launches += 1;
+    for (int i = 0; i < n; ++i) cache->empty[seqs[i]] = 0;
+    return launch_pack<false>(cache, a, list, stream);
+}
+
+kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, const int32_t *seqs, int32_t n_groups, int32_t n_q_heads,
+                               void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_cache_share");
+    if (!cache) return KVZAP_ERR_INVALID_ARG;
+    kvzap_ctx *ctx = cache->ctx;
+    begin_op(ctx);
+    const kvzap_config &c = ctx->cfg;
+    const CacheView &v = cache->v;
+    if (n_groups < 0 || (n_groups > 0 && (!group_start || !seqs)))
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start and seqs (host), n_groups >= 0 are required");
+    if (n_q_heads < c.n_kv_heads || n_q_heads % c.n_kv_heads != 0 || n_q_heads / c.n_kv_heads > kAttnMaxGroup)
+        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: n_q_heads must be 1..%d times the number of KV heads", kAttnMaxGroup);
+    if ((c.head_dim != 64 && c.head_dim != 128) || v.page_tokens % kAttnTileRows != 0 || v.window % kAttnTileRows != 0)
+        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: head_dim 64 or 128, page_tokens and window multiples of %d are required", kAttnTileRows);
+    int32_t n_members = 0;
+    if (n_groups > 0) {
+        if (group_start[0] != 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start begins with 0");
+        for (int g = 0; g < n_groups; ++g)
+            if (group_start[g + 1] < group_start[g] || group_start[g + 1] > v.n_seqs)
+                return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start does not ascend to at most n_seqs");
+        n_members = group_start[n_groups];
+    }
+    kvzap_status st = check_slots(cache, "share", seqs, n_members, true);
+    if (st != KVZAP_OK) return st;
+    DeviceGuard guard(c.device);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const int group = n_q_heads / c.n_kv_heads;
+    const size_t B = static_cast<size_t>(v.n_seqs);
+    // Groups of more members than 256 rows of queries hold are cut into equal parts; of one member there is nothing to share.
+    const int most = 256 / group;
+    std::vector<int32_t> meta;
+    int32_t n_subs = 0, rows_max = 0;
+    try {
+        meta.assign(1 + (B + 1) + 3 * B, 0);
+        int32_t *start = meta.data() + 1, *member = start + B + 1, *sub = member + B, *pos = sub + B;
+        int32_t at = 0;
+        for (int g = 0; g < n_groups; ++g) {
+            const int m = group_start[g + 1] - group_start[g], parts = (m + most - 1) / most;
+            if (m < 2) continue;
+            for (int i = 0; i < parts; ++i) {
+                const int a = group_start[g] + static_cast<int>(static_cast<int64_t>(m) * i / parts);
+                const int b = group_start[g] + static_cast<int>(static_cast<int64_t>(m) * (i + 1) / parts);
+                start[n_subs] = at;
+                for (int j = a; j < b; ++j) { sub[seqs[j]] = n_subs; pos[seqs[j]] = j - a; member[at++] = seqs[j]; }
+                rows_max = std::max(rows_max, (b - a) * group);
+                n_subs += 1;
+            }
+        }
+        start[n_subs] = at;
+    } catch (...) {
+        return fail(ctx, KVZAP_ERR_CUDA, "out of host memory");
+    }
+    cache->share_subs = 0;
+    if (!cache->share_meta) {
+        KVZAP_CUDA(ctx, cudaMalloc(&cache->share_meta, sizeof(int32_t) * meta.size()));
+        KVZAP_CUDA(ctx, cudaMemsetAsync(cache->share_meta, 0, sizeof(int32_t), stream));
+    }
+    if (!cache->share_tile0)
+        KVZAP_CUDA(ctx, cudaMalloc(&cache->share_tile0, sizeof(int32_t) * (static_cast<size_t>(cache->n_lists) + 1)));
+    KVZAP_CUDA(ctx, cudaMemsetAsync(v.share_rows, 0, sizeof(int32_t) * static_cast<size_t>(cache->n_lists), stream));
+    meta[0] = ++cache->share_stamp;
+    // from pageable host memory: staged by the driver before the call returns
+    KVZAP_CUDA(ctx, cudaMemcpyAsync(cache->share_meta, meta.data(), sizeof(int32_t) * meta.size(), cudaMemcpyHostToDevice, stream));
+    if (n_subs == 0) return KVZAP_OK;
+    // Slots for the pieces that a launch leaves behind; a call of more layers than there is room for takes them in turns, so that what one launch
+    // leaves is still in the L2 when the next one reads it.
+    constexpr size_t kSlotsBytes = size_t{64} << 20;
+    const size_t slot_bytes = static_cast<size_t>(rows_max) * (sizeof(float) * c.head_dim + sizeof(float2));
+    const size_t per_layer = static_cast<size_t>(n_subs) * c.n_kv_heads;
+    size_t layers = kSlotsBytes / slot_bytes > static_cast<size_t>(ctx->sm_count) ? (kSlotsBytes / slot_bytes - ctx->sm_count) / per_layer : 0;
+    layers = std::min(std::max(layers, size_t{1}), static_cast<size_t>(c.n_layers));
+    const size_t need = (ctx->sm_count + layers * per_layer) * slot_bytes;
+    if (need > cache->share_part_bytes) {
+        KVZAP_CUDA(ctx, cudaFree(cache->share_part));               // waits for the launches that use it
+        cache->share_part = nullptr;
+        cache->share_part_bytes = 0;
+        KVZAP_CUDA(ctx, cudaMalloc(&cache->share_part, need));
+        cache->share_part_bytes = need;
+    }
+    if (cache->share_box == 0) {
+        int32_t box = kAttnTileRows;
+        while (box < kShTile && v.page_tokens % (2 * box) == 0) box *= 2;
+        const uint64_t rows = static_cast<uint64_t>(v.n_pages_pool) * v.page_tokens;
+        if (rows >= (uint64_t{1} << 31) || rows < static_cast<uint64_t>(box))
+            return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: the pools must have fewer than 2^31 rows, and a page");
+        st = make_tmap(ctx, &cache->tm_kshare, v.k_pool, rows, c.head_dim, static_cast<uint32_t>(box));
+        if (st == KVZAP_OK) st = make_tmap(ctx, &cache->tm_vshare, v.v_pool, rows, c.head_dim, static_cast<uint32_t>(box));
+        if (st != KVZAP_OK) return st;
+        KVZAP_CUDA(ctx, cudaFuncSetAttribute(shared_kernel(c.head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(sh_smem_bytes(c.head_dim))));
+        cache->share_box = box;
+    }
+    const int32_t *start = cache->share_meta + 1, *member = start + B + 1;
+    const unsigned units = static_cast<unsigned>(static_cast<size_t>(c.n_layers) * per_layer);
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    make_launch(&cfg, attrs, dim3(units), dim3(32), 0, stream, false, 1);
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share_count_kernel, v, start, member, static_cast<int>(n_subs), cache->share_tile0));
+    share_scan_kernel<<<1, 1024, 0, stream>>>(cache->share_tile0, static_cast<int>(units));
+    KVZAP_CUDA(ctx, cudaGetLastError());
+    ctx->launches += 2;
+    cache->share_subs = n_subs;
+    cache->share_q_heads = n_q_heads;
+    cache->share_rows_max = rows_max;
+    cache->share_layers = static_cast<int32_t>(layers);
+    return KVZAP_OK;
+}
+
+kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end, const void *Q,
+                                           int32_t n_q_heads, float scale, void *O, void *stream_)
+{
+    NvtxRange nvtx_range("kvzap_decode_attention_shared");
+    if (!ctx || !cache || cache->ctx != ctx) return KVZAP_ERR_INVALID_ARG;
+    if (cache->share_subs == 0) return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, false);
+    begin_op(ctx);
+    const kvzap_config &c = ctx->cfg;
+    const CacheView &v = cache->v;
+    DeviceGuard guard(c.device);
+    kvzap_status st = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, false);
+    if (st != KVZAP_OK) return st;
+    if (n_q_heads != cache->share_q_heads)
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "attention: the groups were told for %d query heads (kvzap_cache_share)", cache->share_q_heads);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    SharedAttnParams p;
+    memset(&p, 0, sizeof p);
+    const size_t B = static_cast<size_t>(v.n_seqs);
+    p.c = v;
+    p.sub_start = cache->share_meta + 1;
+    p.sub_seqs = p.sub_start + B + 1;
+    p.v.seq_sub = p.sub_seqs + B;
+    p.v.seq_pos = p.v.seq_sub + B;
+    p.v.tile0 = cache->share_tile0;
+    p.v.n_subs = cache->share_subs;
+    p.v.rows_max = cache->share_rows_max;
+    p.v.n_ctas = ctx->sm_count;
+    p.v.stamp_now = cache->share_meta;
+    p.v.stamp = cache->share_stamp;
+    p.group = n_q_heads / c.n_kv_heads;
+    p.box_rows = cache->share_box;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.status = ctx->status_dev;
+    const size_t layer_bytes = B * n_q_heads * c.head_dim * 2;
+    for (int32_t l0 = layer_begin; l0 < layer_end; l0 += cache->share_layers) {
+        const int32_t l1 = std::min(layer_end, l0 + cache->share_layers);
+        const uint8_t *q = static_cast<const uint8_t *>(Q) + static_cast<size_t>(l0 - layer_begin) * layer_bytes;
+        uint8_t *o = static_cast<uint8_t *>(O) + static_cast<size_t>(l0 - layer_begin) * layer_bytes;
+        p.layer0 = l0;
+        p.n_layers_call = l1 - l0;
+        p.q = reinterpret_cast<const uint16_t *>(q);
+        const size_t slots = static_cast<size_t>(ctx->sm_count) + static_cast<size_t>(l1 - l0) * cache->share_subs * c.n_kv_heads;
+        p.v.part = static_cast<const float *>(cache->share_part);
+        p.v.part_ml = reinterpret_cast<const float2 *>(p.v.part + slots * cache->share_rows_max * c.head_dim);
+        {
+            ProfScope prof(ctx, KVZAP_KERNEL_ATTENTION, stream);
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attrs[2];
+            make_launch(&cfg, attrs, dim3(static_cast<unsigned>(ctx->sm_count)), dim3(kShThreads), sh_smem_bytes(c.head_dim), stream,
+                        !ctx->profiling, 1);
+            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, shared_kernel(c.head_dim), cache->tm_kshare, cache->tm_vshare, p));
+        }
+        ctx->launches += 1;
+        st = attention_impl(ctx, cache, l0, l1, q, n_q_heads, scale, o, stream_, false, &p.v);
+        if (st != KVZAP_OK) return st;
+    }
     return KVZAP_OK;
 }
 
@@ -3027,6 +3569,14 @@ kvzap_status kvzap_cache_import(kvzap_cache *cache, const int32_t *prefix_len, c
     KVZAP_CUDA(ctx, cudaMemcpyAsync(cache->v.page_cursor, &next_free_page, sizeof(int32_t), cudaMemcpyHostToDevice, stream));
     KVZAP_CUDA(ctx, cudaMemsetAsync(cache->v.free_top, 0, sizeof(int32_t), stream));
     KVZAP_CUDA(ctx, cudaMemsetAsync(cache->v.active, 1, static_cast<size_t>(cache->v.n_seqs), stream));
+    KVZAP_CUDA(ctx, cudaMemsetAsync(cache->v.share_rows, 0, sizeof(int32_t) * n, stream));
+    if (cache->v.n_pages_pool > 0) {
+        KVZAP_CUDA(ctx, cudaMemsetAsync(cache->v.page_refs, 0, sizeof(int32_t) * static_cast<size_t>(cache->v.n_pages_pool), stream));
+        count_refs_kernel<<<static_cast<unsigned>(n), 256, 0, stream>>>(cache->v);
+        count_refs_end_kernel<<<static_cast<unsigned>((cache->v.n_pages_pool + 255) / 256), 256, 0, stream>>>(cache->v);
+        KVZAP_CUDA(ctx, cudaGetLastError());
+    }
+    std::fill(cache->empty.begin(), cache->empty.end(), 0);
     KVZAP_CUDA(ctx, cudaStreamSynchronize(stream));
     return KVZAP_OK;
 }
@@ -3132,6 +3682,7 @@ kvzap_status kvzap_prefill_to_cache(kvzap_ctx *ctx, kvzap_cache *cache, int32_t 
     // chunk pushes out of the present window are decided by their buffered scores and appended to the
     // prefix, the chunk's last tokens take their ring slots; then the chunk's kept tokens are appended
     // behind what the lists hold by then.
+    cache->empty[seq] = 0;
     uint32_t *mask = next_mask_slice(ctx);
     st = launch_score(ctx, layer, 1, hidden, n_tokens, scores_out, mask, nullptr, 1, tau, v.window, stream, 0, nullptr, nullptr, nullptr,
                       nullptr, nullptr, false, nullptr, v.window > 0);
@@ -3171,6 +3722,7 @@ kvzap_status kvzap_prefill_to_cache_batch(kvzap_ctx *ctx, kvzap_cache *cache, in
     if (!hidden || !K || !V || !scores_out || !aligned16(hidden) || !aligned16(K) || !aligned16(V))
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "prefill_to_cache_batch: hidden, K, V, scores_out must be non-NULL, aligned");
     DeviceGuard guard(c.device);
+    for (int i = 0; i < n_seqs; ++i) cache->empty[seq_ids[i]] = 0;
     uint32_t *mask = next_mask_slice(ctx);
     st = launch_score(ctx, layer, 1, hidden, n_tokens, scores_out, mask, cu_seqlens, n_seqs, tau, v.window, stream, 0, nullptr, nullptr,
                       nullptr, nullptr, nullptr, false, nullptr, v.window > 0);

@@ -1,0 +1,327 @@
+// Whole sequences of the decode cache: released, forked, packed and unpacked.
+//
+// Forked sequences share pages.  A page of a list that is full is never written again (rows are only appended behind a
+// list's end), so several lists may have it in their tables; page_refs[p] counts the owners of page p beyond the first.
+// Nothing on the decode path touches the counts: a page fresh from the allocator has one owner and a count of zero.
+// Only the last, partly filled page of a list and its window are the list's own and are copied.
+//
+// A release counts each page down and hands back the ones that had no other owner.  Of several owners that go at the same
+// time exactly one finds the count at zero.
+#pragma once
+
+#include "decode_kernels.cuh"
+
+namespace kvzap {
+
+constexpr int kSlotBatch = 256;          // slots (pairs of them) per launch, by value
+struct SlotList { int32_t slot[kSlotBatch]; };
+// dst[i] becomes a copy of src[i]; first[i]: how many of the launch's pairs have this source, at the first of them, 0 at the others
+struct SlotPairs { int32_t src[kSlotBatch], dst[kSlotBatch], first[kSlotBatch]; };
+
+// The pages of lists (seq, *, *), one warp each, go onto the stack of released pages, apart from those that other lists hold
+// too; the lists become empty.  Runs alone on the stream (it is the one kernel that adds to the stack).
+__global__ void __launch_bounds__(32)
+release_seqs_kernel(const CacheView c, const __grid_constant__ SlotList seqs)
+{
+    griddep_wait();              // and lets nothing start before it is done
+    const int32_t seq = seqs.slot[blockIdx.y];
+    const int64_t li = static_cast<int64_t>(seq) * c.n_layers * c.n_heads + blockIdx.x;
+    const int lane = threadIdx.x;
+    const int32_t n_pages = (c.prefix_len[li] + c.page_tokens - 1) / c.page_tokens;
+    const int32_t *table = c.page_table + li * c.max_pages;
+    for (int32_t i0 = 0; i0 < n_pages; i0 += 1024) {             // 32 pages a lane
+        uint32_t mine = 0u;
+        for (int j = 0; j < 32 && i0 + j * 32 < n_pages; ++j) {
+            const int32_t i = i0 + j * 32 + lane;
+            if (i >= n_pages) break;
+            const int32_t page = table[i];
+            if (page < 0 || page >= c.n_pages_pool) continue;    // imported tables may hold anything
+            bool free = __ldcg(c.page_refs + page) == 0;         // nobody else can add to it or take it away
+            if (!free && atomicSub(c.page_refs + page, 1) == 0) {
+                c.page_refs[page] = 0;                           // the other owners went in the meantime
+                free = true;
+            }
+            if (free) mine |= 1u << j;
+        }
+        __syncwarp();
+        int incl = __popc(mine);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        const int total = __shfl_sync(0xffffffffu, incl, 31);
+        int32_t base = 0;
+        if (lane == 0 && total > 0) base = atomicAdd(c.free_top, total);
+        base = __shfl_sync(0xffffffffu, base, 0) + incl - __popc(mine);
+        for (; mine != 0u; mine &= mine - 1u) c.free_stack[base++] = table[i0 + (__ffs(mine) - 1) * 32 + lane];
+    }
+    __syncwarp();
+    if (lane == 0) {
+        c.prefix_len[li] = 0;
+        c.n_tokens[li] = 0;
+        c.share_rows[li] = 0;
+        if (blockIdx.x == 0) c.active[seq] = 0;
+    }
+}
+
+// Owners of each page after an import: counted, then one less (none stays none).
+__global__ void __launch_bounds__(256) count_refs_kernel(const CacheView c)
+{
+    const int64_t li = blockIdx.x;
+    const int32_t n_pages = min((c.prefix_len[li] + c.page_tokens - 1) / c.page_tokens, c.max_pages);
+    for (int32_t i = threadIdx.x; i < n_pages; i += 256) {
+        const int32_t page = c.page_table[li * c.max_pages + i];
+        if (page >= 0 && page < c.n_pages_pool) atomicAdd(c.page_refs + page, 1);
+    }
+}
+__global__ void __launch_bounds__(256) count_refs_end_kernel(const CacheView c)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i < c.n_pages_pool) c.page_refs[i] = max(c.page_refs[i] - 1, 0);
+}
+
+// n 16-byte units from each of two sources to each of two destinations by n_threads threads, of which this is number `at`
+// (at >= n_threads: none).  kBatch loads of either are out before the first store.
+constexpr int kCopyBatch = 4;
+__device__ __forceinline__ void copy_units(uint4 *__restrict__ kd, uint4 *__restrict__ vd, const uint4 *__restrict__ ks,
+                                           const uint4 *__restrict__ vs, int n, int at, int n_threads)
+{
+    for (int i = at; i < n; i += n_threads * kCopyBatch) {
+        uint4 a[kCopyBatch], b[kCopyBatch];
+#pragma unroll
+        for (int j = 0; j < kCopyBatch; ++j)
+            if (i + j * n_threads < n) { a[j] = __ldcg(ks + i + j * n_threads); b[j] = __ldcg(vs + i + j * n_threads); }
+#pragma unroll
+        for (int j = 0; j < kCopyBatch; ++j)
+            if (i + j * n_threads < n) { kd[i + j * n_threads] = a[j]; vd[i + j * n_threads] = b[j]; }
+    }
+}
+
+// One CTA per pair and list (pairs fastest: the children of one list read it at the same time): the table's whole pages, the
+// rows behind them into a page of the child's own, the window.  Bound by writing the windows.
+constexpr int kForkThreads = 256;
+__global__ void __launch_bounds__(kForkThreads)
+fork_kernel(const CacheView c, const __grid_constant__ SlotPairs pairs, int32_t *__restrict__ status)
+{
+    griddep_wait();
+    __shared__ int32_t page_s;
+    const int pair = blockIdx.x;
+    const int64_t each = static_cast<int64_t>(c.n_layers) * c.n_heads;
+    const int64_t from = pairs.src[pair] * each + blockIdx.y, to = pairs.dst[pair] * each + blockIdx.y;
+    const int32_t n_prefix = c.prefix_len[from], n_tokens = c.n_tokens[from];
+    const int32_t whole = n_prefix / c.page_tokens, tail = n_prefix - whole * c.page_tokens;
+    if (threadIdx.x == 0) {
+        const int32_t page = tail > 0 ? cache_take_page(c, status) : -1;
+        page_s = page;
+        if (page >= 0) c.page_table[to * c.max_pages + whole] = page;
+        // without a page the rows behind the whole ones are lost, as a step loses the row that finds none
+        c.prefix_len[to] = tail > 0 && page < 0 ? whole * c.page_tokens : n_prefix;
+        c.n_tokens[to] = n_tokens;
+        c.share_rows[to] = 0;
+        if (blockIdx.y == 0) c.active[pairs.dst[pair]] = c.active[pairs.src[pair]];
+    }
+    const int32_t more = pairs.first[pair];
+    for (int32_t i = threadIdx.x; i < whole; i += kForkThreads) {
+        const int32_t page = c.page_table[from * c.max_pages + i];
+        c.page_table[to * c.max_pages + i] = page;
+        if (more > 0 && page >= 0 && page < c.n_pages_pool) atomicAdd(c.page_refs + page, more);
+    }
+    // the ring's valid slots, in place: slot n % window is that of token n in either ring
+    const int32_t n_ring = min(n_tokens, c.window);
+    const int64_t fr = from * c.window, tr = to * c.window;
+    for (int32_t i = threadIdx.x; i < n_ring; i += kForkThreads) c.score_ring[tr + i] = c.score_ring[fr + i];
+    copy_units(c.k_ring + tr * c.row_units, c.v_ring + tr * c.row_units, c.k_ring + fr * c.row_units, c.v_ring + fr * c.row_units,
+               n_ring * c.row_units, threadIdx.x, kForkThreads);
+    __syncthreads();
+    const int32_t page = page_s;
+    if (page < 0) return;
+    const int64_t src = static_cast<int64_t>(c.page_table[from * c.max_pages + whole]) * c.page_tokens * c.row_units;
+    const int64_t dst = static_cast<int64_t>(page) * c.page_tokens * c.row_units;
+    copy_units(c.k_pool + dst, c.v_pool + dst, c.k_pool + src, c.v_pool + src, tail * c.row_units, threadIdx.x, kForkThreads);
+}
+
+// ---------------------------------------------------------------- packed sequences
+// The lists of slots seqs[0 .. n), in the order (slot, layer, head), as dense rows one list after the other: list i is rows
+// [row_start[i], row_start[i + 1]), its paged rows first, then its window, oldest first.  Beside the rows: n_tokens[i] (tokens
+// appended so far, by which a window's slots go round) and the scores of the window's tokens, oldest first, zeros behind.
+struct PackArgs {
+    CacheView c;
+    uint4 *K, *V;                        // [capacity_rows][row_units]
+    int64_t capacity_rows;
+    int64_t *row_start;                  // [n_lists + 1]
+    int32_t *n_tokens;                   // [n_lists]
+    float *scores;                       // [n_lists][window] or nullptr
+    int32_t n_lists;
+    int32_t *status;
+};
+
+constexpr int kPackThreads = 256;
+constexpr int kPackRows = 64;            // rows that a warp moves at a time: 2 a lane look up where they are
+constexpr int kPackLists = 24576;        // lists of a launch: their starts are in shared memory
+
+// Where this list's rows are: `slot` names the list among the cache's.
+__device__ __forceinline__ int64_t pack_list(const CacheView &c, const SlotList &seqs, int32_t i)
+{
+    const int32_t each = c.n_layers * c.n_heads;
+    return static_cast<int64_t>(seqs.slot[i / each]) * each + i % each;
+}
+
+// Exclusive running sums of v(i), i < n, in sums[0 .. n], by the whole CTA.
+template <typename F>
+__device__ __forceinline__ void cta_sums(int64_t *sums, int n, F v)
+{
+    __shared__ int64_t warp_s[kPackThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = (n + kPackThreads - 1) / kPackThreads, first = threadIdx.x * per;
+    int64_t mine = 0;
+    for (int i = first; i < first + per && i < n; ++i) mine += v(i);
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    if (lane == 31) warp_s[warp] = incl;
+    __syncthreads();
+    int64_t at = incl - mine;
+    for (int w = 0; w < warp; ++w) at += warp_s[w];
+    for (int i = first; i < first + per && i < n; ++i) { sums[i] = at; at += v(i); }
+    if (threadIdx.x == kPackThreads - 1) sums[n] = at;
+    __syncthreads();
+}
+
+// kOut: lists -> packed rows, else packed rows -> lists (whose tables, lengths and counts are there already).  Every CTA sums the
+// lists' lengths up itself and takes an equal share of all rows, whatever the lists' own lengths; a warp takes kPackRows rows at a
+// time: each lane finds two rows' places (list, page), then the rows' 16-byte units are moved by all lanes.
+template <bool kOut>
+__global__ void __launch_bounds__(kPackThreads)
+pack_kernel(const PackArgs a, const __grid_constant__ SlotList seqs)
+{
+    griddep_wait();
+    extern __shared__ int64_t start_s[];                       // [n_lists + 1]
+    const CacheView &c = a.c;
+    const int n = a.n_lists, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (kOut) {
+        cta_sums(start_s, n, [&](int i) {
+            const int64_t li = pack_list(c, seqs, i);
+            return static_cast<int64_t>(c.prefix_len[li]) + min(c.n_tokens[li], c.window);
+        });
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x; i <= n; i += static_cast<int64_t>(gridDim.x) * kPackThreads) {
+            a.row_start[i] = start_s[i];
+            if (i < n) a.n_tokens[i] = c.n_tokens[pack_list(c, seqs, static_cast<int32_t>(i))];
+        }
+    } else {
+        for (int i = threadIdx.x; i <= n; i += kPackThreads) start_s[i] = a.row_start[i];
+        __syncthreads();
+    }
+    if (a.scores != nullptr && c.window > 0) {
+        const int64_t total = static_cast<int64_t>(n) * c.window;
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPackThreads + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * kPackThreads) {
+            const int32_t which = static_cast<int32_t>(i / c.window), at = static_cast<int32_t>(i % c.window);
+            const int64_t li = pack_list(c, seqs, which);
+            const int32_t tokens = c.n_tokens[li], n_win = min(tokens, c.window);
+            float *ring = c.score_ring + li * c.window + (tokens - n_win + at) % c.window;
+            if (kOut) a.scores[i] = at < n_win ? *ring : 0.0f;
+            else if (at < n_win) *ring = a.scores[i];
+        }
+    }
+    // equal shares of all rows, in whole warps' pieces
+    const int64_t rows = min(start_s[n], a.capacity_rows);
+    const int64_t pieces = (rows + kPackRows - 1) / kPackRows;
+    const int64_t n_warps = static_cast<int64_t>(gridDim.x) * (kPackThreads / 32);
+    for (int64_t piece = static_cast<int64_t>(blockIdx.x) * (kPackThreads / 32) + warp; piece < pieces; piece += n_warps) {
+        const int64_t row0 = piece * kPackRows;
+        const int n_rows = static_cast<int>(min(static_cast<int64_t>(kPackRows), rows - row0));
+        int lo = 0, hi = n;                                      // the list of the piece's first row
+        while (lo + 1 < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (start_s[mid] <= row0) lo = mid; else hi = mid;
+        }
+        // this lane's rows: lane and lane + 32 of the piece; in the pools (>= 0) or the rings (-1 - row); kNone: nowhere
+        constexpr int64_t kNone = INT64_MIN;
+        int64_t at[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t row = row0 + lane + 32 * j;
+            at[j] = kNone;
+            if (lane + 32 * j >= n_rows) continue;
+            while (lo + 1 < n && start_s[lo + 1] <= row) ++lo;
+            const int64_t li = pack_list(c, seqs, lo);
+            const int64_t r = row - start_s[lo];
+            const int32_t n_prefix = c.prefix_len[li], tokens = c.n_tokens[li], n_win = min(tokens, c.window);
+            // a list that found too few pages has lost the rows between its prefix and its window
+            const int64_t in_win = kOut ? r - n_prefix : r - (start_s[lo + 1] - start_s[lo] - n_win);
+            if (in_win >= 0) {
+                if (in_win < n_win) at[j] = -1 - (li * c.window + (tokens - n_win + static_cast<int32_t>(in_win)) % c.window);
+            } else if (r >= 0 && r < n_prefix) {
+                const int32_t page_i = static_cast<int32_t>(r / c.page_tokens);
+                at[j] = static_cast<int64_t>(c.page_table[li * c.max_pages + page_i]) * c.page_tokens + (r - static_cast<int64_t>(page_i) * c.page_tokens);
+            }
+        }
+        const int units = n_rows * c.row_units;
+        const int64_t packed0 = row0 * c.row_units;
+        constexpr int kBatch = 4;
+        for (int u0 = 0; u0 < units; u0 += 32 * kBatch) {
+            uint4 k[kBatch], v[kBatch];
+            int64_t place[kBatch];                               // of the unit in its pool or ring
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int u = u0 + j * 32 + lane;
+                const int r = min(u / c.row_units, kPackRows - 1), in_row = u % c.row_units;
+                const int64_t p0 = __shfl_sync(0xffffffffu, at[0], r & 31), p1 = __shfl_sync(0xffffffffu, at[1], r & 31);
+                const int64_t p = r < 32 ? p0 : p1;
+                place[j] = u < units ? p : kNone;
+                if (place[j] == kNone) continue;
+                place[j] = p >= 0 ? p * c.row_units + in_row : -1 - ((-1 - p) * c.row_units + in_row);
+                if (kOut) {
+                    k[j] = p >= 0 ? __ldcg(c.k_pool + place[j]) : __ldcg(c.k_ring - 1 - place[j]);
+                    v[j] = p >= 0 ? __ldcg(c.v_pool + place[j]) : __ldcg(c.v_ring - 1 - place[j]);
+                } else {
+                    k[j] = __ldcs(a.K + packed0 + u);
+                    v[j] = __ldcs(a.V + packed0 + u);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (place[j] == kNone) continue;
+                if (kOut) {
+                    __stcs(a.K + packed0 + u0 + j * 32 + lane, k[j]);
+                    __stcs(a.V + packed0 + u0 + j * 32 + lane, v[j]);
+                } else if (place[j] >= 0) {
+                    c.k_pool[place[j]] = k[j];
+                    c.v_pool[place[j]] = v[j];
+                } else {
+                    c.k_ring[-1 - place[j]] = k[j];
+                    c.v_ring[-1 - place[j]] = v[j];
+                }
+            }
+        }
+    }
+}
+
+// Pages, lengths and counts of lists that are about to be unpacked (empty, released before), one warp each.
+__global__ void __launch_bounds__(32)
+unpack_pages_kernel(const PackArgs a, const __grid_constant__ SlotList seqs)
+{
+    griddep_wait();
+    const CacheView &c = a.c;
+    const int i = blockIdx.x, lane = threadIdx.x;
+    const int64_t li = pack_list(c, seqs, i);
+    const int64_t rows = a.row_start[i + 1] - a.row_start[i];
+    int32_t tokens = max(a.n_tokens[i], 0);
+    if (rows < min(tokens, c.window)) tokens = rows > 0 ? static_cast<int32_t>(rows) : 0;      // a window has as many rows as are given
+    const int64_t paged = max(rows - min(tokens, c.window), int64_t{0});
+    const int64_t want = (paged + c.page_tokens - 1) / c.page_tokens;
+    int32_t n = static_cast<int32_t>(want < c.max_pages ? want : c.max_pages);
+    n = cache_take_pages(c, a.status, n, c.page_table + li * c.max_pages, lane);
+    if (lane == 0) {
+        if (n < want) atomicCAS(a.status, 0, 4 /* KVZAP_ERR_OOM_PAGES */);
+        c.prefix_len[li] = static_cast<int32_t>(n < want ? static_cast<int64_t>(n) * c.page_tokens : paged);
+        c.n_tokens[li] = tokens;
+        c.share_rows[li] = 0;
+        if (i % (c.n_layers * c.n_heads) == 0) c.active[seqs.slot[i / (c.n_layers * c.n_heads)]] = 1;
+    }
+}
+
+}  // namespace kvzap

@@ -1,0 +1,180 @@
+// Rotary positions of queries and keys, and the rows of the cache, as the projection leaves them.
+//
+// Element pairs (x1, x2) of a head -- (i, i + R/2), or neighbours (2i, 2i + 1) -- turn by the token's position times the pair's
+// frequency f_i:  y1 = (x1 cos - x2 sin) a,  y2 = (x2 cos + x1 sin) a,  a = the magnitude; the inverse (also the gradient) turns
+// the other way.  Elements from R on are left as they are.
+//
+// The angle is kept as a fraction of a turn in 64-bit fixed point: step_i = f_i / 2 pi * 2^64, and position * step_i modulo
+// 2^64 is the fraction, exactly (whole turns drop out by themselves; what is off is the step, 2^-53 of it).  Its upper 32 bits, a
+// signed multiple of 2^-31 half turns, go to sincospif: an angle is off by 2^-32 turns + the rounding to fp32, at any position,
+// without a 64-bit sine and without a table of positions.
+//
+// Bound by reading each row once and writing it once.  A thread has 8 pairs (two 16-byte pieces of a head) of one token, works
+// their sines out once and goes over the token's heads, of all tensors of the call, with them.
+//
+// 8-bit rows (D E4M3 codes, then the fp32 scale and 12 zero bytes): scale = the row's largest magnitude / 448 (1 for a row of
+// zeros), codes rounded to nearest from the fp32 result, which is rounded nowhere before.
+#pragma once
+
+#include "ptx.cuh"
+
+namespace kvzap {
+
+constexpr int kRotTensors = 3;
+constexpr int kRotThreads = 256;
+constexpr uint32_t kRotRotate = 1u, kRotRows8 = 2u;           // as KVZAP_ROWS_*
+
+struct RotaryTensor {
+    const uint8_t *in;
+    uint8_t *out;
+    int64_t in_token, in_head, out_token, out_head;           // bytes
+    int32_t n_heads;
+    uint32_t flags;
+};
+template <int kPairs>
+struct RotaryParams {
+    RotaryTensor t[kRotTensors];
+    const int32_t *positions;
+    int64_t n_tokens;
+    int32_t n_tensors, n_heads;       // heads of all tensors together
+    int32_t head_dim, rotary_dim;
+    int32_t lanes;                    // threads along a head: head_dim / 16
+    int32_t rows;                     // heads that are worked on at a time by the threads of a token
+    float magnitude, sign;
+    uint64_t step[kPairs];            // [rotary_dim / 2] turns a token, in units of 2^-64
+};
+
+__device__ __forceinline__ void rotary_turn(uint64_t step, int32_t position, float magnitude, float sign, float &c, float &s)
+{
+    const uint64_t turn = step * static_cast<uint64_t>(static_cast<int64_t>(position));
+    sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 4.656612873077393e-10f /* 2^-31 */, &s, &c);
+    c *= magnitude;
+    s *= magnitude * sign;
+}
+// two fp32 -> E4M3 codes, lo in the low byte; values beyond the format's largest go to it
+__device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// head_dim and rotary_dim multiples of 16, everything 16-byte aligned.
+template <int kPairs, bool kInterleaved>
+__global__ void __launch_bounds__(kRotThreads)
+rotary_kernel(const __grid_constant__ RotaryParams<kPairs> p)
+{
+    griddep_wait();                   // and lets nothing start before it is done: its outputs are the next call's inputs
+    const int per_token = p.lanes * p.rows;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kRotThreads + threadIdx.x;
+    const int64_t token = at / per_token;
+    const int in_token = static_cast<int>(at - token * per_token);
+    const int j = in_token % p.lanes, row = in_token / p.lanes;
+    const bool there = token < p.n_tokens;
+    const int turning = p.rotary_dim / 16;                     // threads of a head that turn anything
+    const bool turn = there && j < turning;
+    // first elements of this thread's two pieces
+    int e0, e1;
+    if (j >= turning) { e0 = p.rotary_dim + 16 * (j - turning); e1 = e0 + 8; }
+    else if (kInterleaved) { e0 = 16 * j; e1 = e0 + 8; }
+    else { e0 = 8 * j; e1 = e0 + p.rotary_dim / 2; }
+    float c[8], s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+    if (turn) {
+        const int32_t position = p.positions[token];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rotary_turn(p.step[8 * j + i], position, p.magnitude, p.sign, c[i], s[i]);
+    }
+    int h = row;                                               // head of the call, then of tensor t
+    const int n_rounds = (p.n_heads + p.rows - 1) / p.rows;
+    int ti = 0;
+#pragma unroll 1
+    for (int round = 0; round < n_rounds; ++round, h += p.rows) {
+        // every thread of a warp goes along: rows of 8 bits are worked out by several
+        while (ti < p.n_tensors && h >= p.t[ti].n_heads) { h -= p.t[ti].n_heads; ++ti; }
+        const bool work = there && ti < p.n_tensors;
+        const RotaryTensor &t = p.t[ti < p.n_tensors ? ti : 0];
+        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+        if (work) {
+            const uint8_t *src = t.in + token * t.in_token + h * t.in_head;
+            a = *reinterpret_cast<const uint4 *>(src + 2 * e0);
+            b = *reinterpret_cast<const uint4 *>(src + 2 * e1);
+        }
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+        if (turn && (t.flags & kRotRotate)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float &x1 = x[kInterleaved ? 2 * i : i], &x2 = x[kInterleaved ? 2 * i + 1 : i + 8];
+                const float y1 = x1 * c[i] - x2 * s[i], y2 = x2 * c[i] + x1 * s[i];
+                x1 = y1;
+                x2 = y2;
+            }
+        }
+        uint8_t *dst = t.out + token * t.out_token + h * t.out_head;
+        if (work && !(t.flags & kRotRows8)) {
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+            *reinterpret_cast<uint4 *>(dst + 2 * e0) = make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4 *>(dst + 2 * e1) = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+        if (__any_sync(0xffffffffu, work && (t.flags & kRotRows8))) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+            for (int o = 1; o < p.lanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));      // 4 or 8 lanes a row
+            if (work && (t.flags & kRotRows8)) {
+                const float scale = top > 0.0f ? __fdiv_rn(top, 448.0f) : 1.0f;
+                uint32_t y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[i] = pack_e4m3x2(__fdiv_rn(x[4 * i], scale), __fdiv_rn(x[4 * i + 1], scale)) |
+                           pack_e4m3x2(__fdiv_rn(x[4 * i + 2], scale), __fdiv_rn(x[4 * i + 3], scale)) << 16;
+                *reinterpret_cast<uint2 *>(dst + e0) = make_uint2(y[0], y[1]);
+                *reinterpret_cast<uint2 *>(dst + e1) = make_uint2(y[2], y[3]);
+                if (j == 0) *reinterpret_cast<uint4 *>(dst + p.head_dim) = make_uint4(__float_as_uint(scale), 0u, 0u, 0u);
+            }
+        }
+    }
+}
+
+// Any even rotary_dim, any alignment: a thread per pair (or per element past the rotary ones), bf16 rows.
+template <int kPairs, bool kInterleaved>
+__global__ void __launch_bounds__(kRotThreads)
+rotary_odd_kernel(const __grid_constant__ RotaryParams<kPairs> p)
+{
+    griddep_wait();
+    const int pairs = p.rotary_dim / 2, items = pairs + p.head_dim - p.rotary_dim;
+    const int64_t total = p.n_tokens * items;
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kRotThreads + threadIdx.x; at < total;
+         at += static_cast<int64_t>(gridDim.x) * kRotThreads) {
+        const int64_t token = at / items;
+        const int i = static_cast<int>(at - token * items);
+        float c = 1.0f, s = 0.0f;
+        if (i < pairs) rotary_turn(p.step[i], p.positions[token], p.magnitude, p.sign, c, s);
+        for (int ti = 0; ti < p.n_tensors; ++ti) {
+            const RotaryTensor &t = p.t[ti];
+            for (int h = 0; h < t.n_heads; ++h) {
+                const uint16_t *src = reinterpret_cast<const uint16_t *>(t.in + token * t.in_token + h * t.in_head);
+                uint16_t *dst = reinterpret_cast<uint16_t *>(t.out + token * t.out_token + h * t.out_head);
+                if (i >= pairs) { dst[pairs + i] = src[pairs + i]; continue; }
+                const int e0 = kInterleaved ? 2 * i : i, e1 = kInterleaved ? 2 * i + 1 : i + pairs;
+                const uint16_t b0 = src[e0], b1 = src[e1];
+                if (!(t.flags & kRotRotate)) { dst[e0] = b0; dst[e1] = b1; continue; }
+                const float x1 = __uint_as_float(static_cast<uint32_t>(b0) << 16), x2 = __uint_as_float(static_cast<uint32_t>(b1) << 16);
+                const uint32_t y = pack_bf16x2(x1 * c - x2 * s, x2 * c + x1 * s);
+                dst[e0] = static_cast<uint16_t>(y);
+                dst[e1] = static_cast<uint16_t>(y >> 16);
+            }
+        }
+    }
+}
+
+}  // namespace kvzap

@@ -1,0 +1,660 @@
+// Attention of the new tokens of sequences that share a prefix (forked ones: their lists begin with the same pages).
+//
+// The rows that the members of a group share are taken once for all of them: for each (layer, group, KV head) the members'
+// query heads -- members x G rows of Q -- are one operand of 128 or 256 rows, and every shared row of K and V is read once
+// per launch instead of once per member.  What is a member's own (the rows behind the shared pages, its window) is walked by
+// decode_attn_kernel as ever, which also joins the two parts: softmax over a list that is cut in two is
+//   O = (O1 2^(m1-m) + O2 2^(m2-m)) / (l1 2^(m1-m) + l2 2^(m2-m)),  m = max(m1, m2)
+// with (m, l, O) the running maximum (in powers of two), sum and unnormalised output of either part, all in fp32.
+//
+// With 128 rows of Q a row of K and V (512 bytes at D = 128) costs 65536 operations, half of what the tensor cores do while
+// it is read: up to some 256 rows the kernel is bound by reading the shared rows once, above by the matrix products.
+//
+// One CTA per SM; all shared tiles of the call (128 rows of one list each), in list order, are cut into equal runs, one per
+// CTA, so that lists of any lengths fill the device; a run covers the end of one list, some whole ones, the beginning of
+// another, and each such piece leaves its (m, l, O) in a slot of its own: piece (CTA c, list u) in slot c + u, which no two
+// pieces share (of two pieces one after the other at least one of c and u has grown).  decode_attn_kernel works out from the
+// same numbers which slots a list has.
+//
+// Within a CTA: one warp issues the copies (TMA, 128-byte swizzle, boxes of as many rows as pages allow), one the matrix
+// products (tcgen05: S = Q K^T into tensor memory, O += P V with P from tensor memory), and two groups of four warps do the
+// softmax, a row per thread, each with its own S and O in tensor memory, so that one group's exponentials run beside the
+// other's products.  Up to 128 rows of Q: both groups have the same rows and take every other tile, and are joined at the
+// end of a piece.  Up to 256 rows: each group has its own 128 rows and both take every tile.
+// P overwrites the first half of S; the matrix unit takes a thread's products in order, so the next S, issued behind P V,
+// cannot overtake it.  O is rescaled only when the running maximum has grown by more than 2^8 since the last time (P then
+// stays below 2^8, and its 8 bits are relative): after a few tiles hardly ever.
+#pragma once
+
+#include "decode_kernels.cuh"
+#include "ptx.cuh"
+
+namespace kvzap {
+
+constexpr int kShTile = 128;                 // shared rows per tile, rows of Q per group of warps
+constexpr int kShThreads = 320;              // 2 x 4 softmax warps, producer, products
+constexpr float kShGrow = 8.0f;              // powers of two by which the maximum may grow before O is rescaled
+
+// What decode_attn_kernel needs to find the slots of a list.
+struct ShareView {
+    const int32_t *tile0;                    // [L][n_subs][H] (+ 1) tiles of shared rows before each list, all layers
+    const int32_t *seq_sub, *seq_pos;        // [n_seqs] the group that a sequence is in and its place there
+    const float *part;                       // [slot][rows_max][D] unnormalised outputs
+    const float2 *part_ml;                   // [slot][rows_max] (m, l); l < 0: a wait ran out
+    int32_t n_subs, rows_max, n_ctas;
+    // Groups told after this call was captured have another stamp: the call then reads every list by itself.
+    const int32_t *stamp_now;
+    int32_t stamp;
+};
+
+struct SharedAttnParams {
+    CacheView c;
+    ShareView v;
+    int32_t layer0, n_layers_call, group;
+    int32_t box_rows;                        // rows per copy: a power of two, 16..128, that divides the page
+    float scale_log2e;
+    const uint16_t *q;                       // [n_layers_call][B][H * G][D]
+    const int32_t *sub_start, *sub_seqs;     // members of the groups
+    int32_t *status;
+};
+
+// CTAs that take part in a call of so many tiles, and the first tile of CTA i's run.  A piece leaves as many bytes behind as
+// a tile of 128 rows brings in, so a run is at least kShMinTiles tiles, if that leaves SMs idle too.
+constexpr int kShMinTiles = 2;
+__device__ __forceinline__ int share_ctas(int64_t tiles, int n_ctas)
+{
+    const int64_t want = (tiles + kShMinTiles - 1) / kShMinTiles;
+    return static_cast<int>(want < n_ctas ? (want > 0 ? want : 1) : n_ctas);
+}
+__device__ __forceinline__ int64_t share_run(int64_t tiles, int ctas, int i) { return tiles * i / ctas; }
+// the CTA whose run tile t is in
+__device__ __forceinline__ int share_owner(int64_t tiles, int ctas, int64_t t) { return static_cast<int>(((t + 1) * ctas - 1) / tiles); }
+
+__host__ __device__ constexpr int sh_stages(int d) { return d == 128 ? 5 : 9; }
+__host__ __device__ constexpr uint32_t sh_stage_bytes(int d) { return kShTile * d * 2u; }
+__host__ __device__ constexpr uint32_t sh_smem_bytes(int d)
+{
+    return 1024u + sh_stages(d) * sh_stage_bytes(d) + 2u * sh_stage_bytes(d) /* Q */ + 512u /* barriers */;
+}
+
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, "
+        "%25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+        "%26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+        "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_x2(uint32_t taddr, uint32_t (&r)[2])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_x2(uint32_t taddr, const uint32_t (&r)[2])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "r"(r[0]), "r"(r[1]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// keeps uses of values just loaded from tensor memory behind the wait
+__device__ __forceinline__ void reg_fence32(uint32_t *r)
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i])::"memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A as packed bf16 pairs, one row per lane
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Shared-memory descriptor of a B operand that is N-contiguous in memory (rows of V: k is the row, n the element), written with
+// the 128-byte swizzle: 64 elements of n by 8 rows of k make a 1024-byte block, the next 8 rows follow directly, the next 64
+// elements block_bytes further on.
+__device__ __forceinline__ uint64_t umma_desc_n_major_sw128(uint32_t smem_addr, uint32_t block_bytes)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(block_bytes >> 4) << 16;        // between 64-element blocks along n
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;               // between 8-row groups along k
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+constexpr uint32_t kIdescBNMajor = 1u << 16;                   // instruction descriptor: B is N-contiguous
+
+__device__ __forceinline__ void st_global_v8(float *p, const float *v)
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
+}
+
+// ---------------------------------------------------------------- what a group shares
+// One warp per (layer, group, head): the number of leading pages that the lists of all its members have in common, by comparing
+// their tables, whole pages only.  Members whose slot holds no sequence are left out.  rows of a member's list that are read
+// with the group go to c.share_rows; tiles to n_tiles.  Fewer rows than a tile are not worth a tile.
+__global__ void __launch_bounds__(32)
+share_count_kernel(const CacheView c, const int32_t *__restrict__ sub_start, const int32_t *__restrict__ sub_seqs, int n_subs,
+                   int32_t *__restrict__ n_tiles)
+{
+    griddep_wait();
+    const int unit = blockIdx.x, lane = threadIdx.x;
+    const int h = unit % c.n_heads, s = unit / c.n_heads % n_subs, l = unit / (c.n_heads * n_subs);
+    const int m0 = sub_start[s], n_mem = sub_start[s + 1] - m0;
+    auto list_of = [&](int m) {
+        return (static_cast<int64_t>(sub_seqs[m0 + m]) * c.n_layers + l) * c.n_heads + h;
+    };
+    int live = 0, leader = -1, pages = INT32_MAX;
+    for (int i0 = 0; i0 < n_mem; i0 += 32) {
+        const int i = i0 + lane;
+        const bool is = i < n_mem && c.active[sub_seqs[m0 + i]] != 0;
+        if (is) pages = min(pages, c.prefix_len[list_of(i)] / c.page_tokens);
+        const uint32_t who = __ballot_sync(0xffffffffu, is);
+        if (leader < 0 && who != 0u) leader = i0 + __ffs(who) - 1;
+        live += __popc(who);
+    }
+    pages = __reduce_min_sync(0xffffffffu, pages);
+    if (live < 2) pages = 0;
+    if (pages > 0) {
+        const int32_t *first = c.page_table + list_of(leader) * c.max_pages;
+        int same = pages;
+        for (int i0 = 0; i0 < pages && same == pages; i0 += 32) {
+            const int i = i0 + lane;
+            bool differs = false;
+            if (i < pages) {
+                const int32_t page = first[i];
+                for (int m = 0; m < n_mem; ++m)
+                    if (c.active[sub_seqs[m0 + m]] != 0 && c.page_table[list_of(m) * c.max_pages + i] != page) { differs = true; break; }
+            }
+            const uint32_t who = __ballot_sync(0xffffffffu, differs);
+            if (who != 0u) same = i0 + __ffs(who) - 1;
+        }
+        pages = same;
+    }
+    int32_t rows = pages * c.page_tokens;
+    if (rows < kShTile) rows = 0;
+    for (int i = lane; i < n_mem; i += 32)
+        if (c.active[sub_seqs[m0 + i]] != 0) c.share_rows[list_of(i)] = rows;
+    if (lane == 0) n_tiles[unit] = (rows + kShTile - 1) / kShTile;
+}
+
+// Exclusive running sums of v[0 .. n), in place, the total in v[n].
+__global__ void __launch_bounds__(1024) share_scan_kernel(int32_t *__restrict__ v, int n)
+{
+    __shared__ int32_t warp_s[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t before = 0;
+    for (int i0 = 0; i0 < n; i0 += 1024) {
+        const int i = i0 + threadIdx.x;
+        const int32_t x = i < n ? v[i] : 0;
+        int32_t incl = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        if (lane == 31) warp_s[warp] = incl;
+        __syncthreads();
+        int32_t at = before;
+        for (int w = 0; w < warp; ++w) at += warp_s[w];
+        int32_t all = before;
+        for (int w = 0; w < 32; ++w) all += warp_s[w];
+        if (i < n) v[i] = at + incl - x;
+        before = all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) v[n] = before;
+}
+
+// ---------------------------------------------------------------- the shared rows
+// A CTA's run of tiles, piece by piece; every warp walks it for itself.
+struct SharePiece {
+    int unit;                       // list of the call: (layer - layer0, group, head)
+    int l, s, h;                    // ... layer within the call
+    int t0, t1;                     // tiles [t0, t1) of the list
+    int m0, n_mem;                  // the group's members
+    int32_t n_rows;                 // shared rows of the list, 0: no member shares any more
+    int64_t leader;                 // list of a member that does
+};
+struct ShareWalk {
+    const SharedAttnParams &p;
+    const int32_t *tile0;           // of the call's first list
+    int64_t base, at, end;          // tile numbers within the call
+    int unit, n_units;
+    __device__ ShareWalk(const SharedAttnParams &p_, int lane) : p(p_)
+    {
+        const int per_layer = p.v.n_subs * p.c.n_heads;
+        n_units = p.n_layers_call * per_layer;
+        tile0 = p.v.tile0 + static_cast<int64_t>(p.layer0) * per_layer;
+        at = end = base = 0;
+        unit = 0;
+        if (*p.v.stamp_now != p.v.stamp) return;
+        base = tile0[0];
+        const int64_t tiles = tile0[n_units] - base;
+        const int ctas = share_ctas(tiles, p.v.n_ctas);
+        if (tiles == 0 || static_cast<int>(blockIdx.x) >= ctas) return;
+        at = share_run(tiles, ctas, blockIdx.x);
+        end = share_run(tiles, ctas, blockIdx.x + 1);
+        // the last list that begins at or before the run: 32 probes a round
+        int lo = 0, hi = n_units;                                   // tile0[lo] - base <= at < tile0[hi] - base
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32;
+            const int probe = lo + lane * step;
+            const bool below = probe < hi && tile0[probe] - base <= at;
+            const int n = __popc(__ballot_sync(0xffffffffu, below));    // the first n probes are (lane 0's always is)
+            const int nlo = lo + (n - 1) * step;
+            hi = min(hi, nlo + step);
+            lo = nlo;
+        }
+        unit = lo;
+    }
+    // Whole warp.  False: the run is over.
+    __device__ bool next(SharePiece &x, int lane)
+    {
+        if (at >= end) return false;
+        while (tile0[unit + 1] - base <= at) ++unit;                // lists without tiles
+        const CacheView &c = p.c;
+        const int64_t first = tile0[unit] - base, last = tile0[unit + 1] - base;
+        x.unit = unit;
+        x.h = unit % c.n_heads;
+        x.s = unit / c.n_heads % p.v.n_subs;
+        x.l = unit / (c.n_heads * p.v.n_subs);
+        x.t0 = static_cast<int>(at - first);
+        x.t1 = static_cast<int>((last < end ? last : end) - first);
+        x.m0 = p.sub_start[x.s];
+        x.n_mem = p.sub_start[x.s + 1] - x.m0;
+        x.n_rows = 0;
+        for (int i0 = 0; i0 < x.n_mem && x.n_rows == 0; i0 += 32) {
+            const int i = i0 + lane;
+            int64_t li = 0;
+            int32_t rows = 0;
+            if (i < x.n_mem) {
+                li = (static_cast<int64_t>(p.sub_seqs[x.m0 + i]) * c.n_layers + p.layer0 + x.l) * c.n_heads + x.h;
+                rows = __ldcg(c.share_rows + li);
+            }
+            const uint32_t who = __ballot_sync(0xffffffffu, rows > 0);
+            if (who == 0u) continue;
+            x.n_rows = __shfl_sync(0xffffffffu, rows, __ffs(who) - 1);
+            x.leader = __shfl_sync(0xffffffffu, li, __ffs(who) - 1);
+        }
+        at = first + x.t1;
+        return true;
+    }
+};
+
+// Ring positions of a piece's operands, in the order of their first use: K0, K1, V0, K2, V1, ..., the last K, V, V.
+__device__ __forceinline__ int sh_k_pos(int t) { return t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ int sh_v_pos(int t, int n) { return t + 1 < n ? 2 * t + 2 : 2 * n - 1; }
+
+template <int kD>
+__global__ void __launch_bounds__(kShThreads, 1)
+shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const SharedAttnParams p)
+{
+    constexpr int kHalves = kD / 64;
+    constexpr int kStages = sh_stages(kD);
+    constexpr uint32_t kStageBytes = sh_stage_bytes(kD);
+    constexpr uint32_t kHalfBytes = kShTile * 128u;
+    extern __shared__ uint8_t sh_smem_raw[];
+    const uint32_t raw_addr = smem_u32(sh_smem_raw);
+    const uint32_t pad = (1024u - (raw_addr & 1023u)) & 1023u;
+    uint8_t *smem = sh_smem_raw + pad;
+    const uint32_t ring = raw_addr + pad;                                   // [kStages] K or V tiles
+    const uint32_t qtile = ring + kStages * kStageBytes;                    // [2] tiles of Q
+    const uint32_t bars = qtile + 2 * kStageBytes;
+    const uint32_t full = bars, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16,
+                   q_full = p_full + 16, done = q_full + 8, o_free = done + 8;
+    __shared__ uint32_t tmem_s;
+    __shared__ volatile int abort_s;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        for (int w = 0; w < 2; ++w) { mbar_init(s_full + 8 * w, 1); mbar_init(p_full + 8 * w, 128); }
+        mbar_init(q_full, 256);
+        mbar_init(done, 1);
+        mbar_init(o_free, 256);
+        abort_s = 0;
+        fence_mbar_init();
+        prefetch_tensormap(&tmap_k);
+        prefetch_tensormap(&tmap_v);
+    }
+    if (warp == 9) {
+        tmem_alloc(smem_u32(&tmem_s), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_s;
+    // Everything ahead of this launch is complete from here on, for the launch behind too, which begins with the members' own rows.
+    griddep_wait();
+    griddep_launch_dependents();
+
+    ShareWalk walk(p, lane);
+    SharePiece x;
+    uint32_t pos0 = 0;                       // ring positions used by the pieces so far
+    bool ok = true;
+    const CacheView &c = p.c;
+
+    if (warp == 8) {
+        // ---- copies.  Lane i: box i / kHalves of the tile, half i % kHalves of its rows
+        const int n_boxes = kShTile / p.box_rows;
+        const int box = lane / kHalves, half = lane % kHalves;
+        const uint64_t policy = l2_policy_evict_first();
+        while (ok && walk.next(x, lane)) {
+            if (x.n_rows == 0) continue;
+            const int n = x.t1 - x.t0;
+            const int32_t *pages = c.page_table + x.leader * c.max_pages;
+            auto row_of = [&](int t) -> int32_t {                           // of this lane's box in the pools, -1: none
+                const int32_t r = (x.t0 + t) * kShTile + box * p.box_rows;
+                if (t >= n || box >= n_boxes || r >= x.n_rows) return -1;
+                const int32_t page_i = r / c.page_tokens;
+                return __ldcg(pages + page_i) * c.page_tokens + (r - page_i * c.page_tokens);
+            };
+            auto copy = [&](const CUtensorMap *map, uint32_t pos, int t, int32_t row) {
+                const uint32_t at = pos0 + pos, stage = at % kStages, round = at / kStages;
+                if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
+                const int rows = min(kShTile, x.n_rows - (x.t0 + t) * kShTile);
+                if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, rows * kD * 2u);
+                __syncwarp();
+                if (row >= 0)
+                    tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * p.box_rows * 128u, map, full + 8 * stage,
+                                half * 64, row, policy);
+            };
+            int32_t cur = row_of(0), next = row_of(1);
+            copy(&tmap_k, 0, 0, cur);
+            for (int t = 0; ok && t < n; ++t) {
+                const int32_t after = row_of(t + 2);
+                if (t + 1 < n) copy(&tmap_k, sh_k_pos(t + 1), t + 1, next);
+                if (ok) copy(&tmap_v, sh_v_pos(t, n), t, cur);
+                cur = next;
+                next = after;
+            }
+            pos0 += 2 * n;
+        }
+    } else if (warp == 9) {
+        // ---- matrix products: S of step i + 2 behind P V of step i
+        const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
+        const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
+        uint32_t n_p[2] = {0u, 0u}, n_piece = 0;
+        while (ok && walk.next(x, lane)) {
+            if (x.n_rows == 0) continue;
+            const int n = x.t1 - x.t0;
+            const bool two = x.n_mem * p.group > 128;
+            const int steps = two ? 2 * n : n;
+            if (!__all_sync(0xffffffffu, mbar_wait(q_full, n_piece & 1, &abort_s))) { ok = false; break; }
+            if (n_piece > 0 && !__all_sync(0xffffffffu, mbar_wait(o_free, (n_piece - 1) & 1, &abort_s))) { ok = false; break; }
+            tc_fence_after_sync();
+            auto tile_of = [&](int i) { return two ? i >> 1 : i; };
+            auto scores = [&](int i) {
+                const int t = tile_of(i), w = i & 1;
+                const uint32_t at = pos0 + sh_k_pos(t), stage = at % kStages;
+                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s))) { ok = false; return; }
+                tc_fence_after_sync();
+                if (lane == 0) {
+                    const uint32_t qa = qtile + (two ? w : 0) * kStageBytes, kb = ring + stage * kStageBytes;
+#pragma unroll
+                    for (int ks = 0; ks < kD / 16; ++ks) {
+                        const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32u;
+                        umma_bf16(tmem + 256 * w, umma_desc_k_major_sw128(qa + off), umma_desc_k_major_sw128(kb + off), idesc_s, ks > 0);
+                    }
+                    umma_commit(s_full + 8 * w);
+                    if (!two || w == 1) umma_commit(empty + 8 * stage);
+                }
+                __syncwarp();
+            };
+            scores(0);
+            if (ok && steps > 1) scores(1);
+            for (int i = 0; ok && i < steps; ++i) {
+                const int t = tile_of(i), w = i & 1;
+                const uint32_t at = pos0 + sh_v_pos(t, n), stage = at % kStages;
+                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s) &&
+                                             mbar_wait(p_full + 8 * w, n_p[w] & 1, &abort_s))) { ok = false; break; }
+                n_p[w] += 1;
+                tc_fence_after_sync();
+                const int rows = min(kShTile, x.n_rows - (x.t0 + t) * kShTile);      // a multiple of 16
+                if (lane == 0) {
+                    const uint32_t vb = ring + stage * kStageBytes;
+                    for (int ks = 0; ks < rows / 16; ++ks)
+                        umma_bf16_ts(tmem + 256 * w + 128, tmem + 256 * w + 8 * ks, umma_desc_n_major_sw128(vb + ks * 2048u, kHalfBytes), idesc_o,
+                                     i > 1 || ks > 0);
+                    if (!two || w == 1) umma_commit(empty + 8 * stage);
+                    if (i + 1 == steps) umma_commit(done);
+                }
+                __syncwarp();
+                if (i + 2 < steps) scores(i + 2);
+            }
+            pos0 += 2 * n;
+            n_piece += 1;
+        }
+    } else {
+        // ---- softmax: thread = row of Q
+        const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
+        uint32_t n_s = 0, n_piece = 0;
+        while (walk.next(x, lane)) {
+            const int n_rows_q = x.n_mem * p.group;
+            const bool two = n_rows_q > 128;
+            const int slot = static_cast<int>(blockIdx.x) + x.unit;
+            const int64_t out_row = static_cast<int64_t>(slot) * p.v.rows_max;
+            float2 *ml_out = const_cast<float2 *>(p.v.part_ml) + out_row;
+            if (!ok) {                                            // a wait ran out: the outputs that this piece is part of are zeros
+                for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
+                if (x.n_rows > 0) named_barrier_sync(1, 256);     // one for each piece that is worked on, whoever gave up when
+                continue;
+            }
+            if (x.n_rows == 0) continue;
+            // Q: 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros
+            {
+                constexpr int kUnits = kD / 8;
+                const int first = two ? w * 128 : 0, n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
+#pragma unroll 4
+                for (int i = at; i < 128 * kUnits; i += n_thr) {
+                    const int r = i / kUnits, u = i % kUnits, qr = first + r;
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (qr < n_rows_q) {
+                        const int m = qr / p.group;
+                        const int64_t b = p.sub_seqs[x.m0 + m];
+                        const int64_t head = (static_cast<int64_t>(x.l) * c.n_seqs + b) * c.n_heads * p.group + x.h * p.group + (qr - m * p.group);
+                        v = __ldg(reinterpret_cast<const uint4 *>(p.q + head * kD) + u);
+                    }
+                    *reinterpret_cast<uint4 *>(smem + kStages * kStageBytes + (two ? w : 0) * kStageBytes + (u >> 3) * kHalfBytes + r * 128 +
+                                               (((u & 7) ^ (r & 7)) << 4)) = v;
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(q_full);
+            }
+            const int n = x.t1 - x.t0, mine = two ? n : (n + 1 - w) / 2;
+            float m_ref = -INFINITY, l_run = 0.0f;
+            for (int i = 0; i < mine; ++i) {
+                const int t = two ? i : 2 * i + w;
+                if (!__all_sync(0xffffffffu, mbar_wait(s_full + 8 * w, n_s & 1, &abort_s))) { ok = false; break; }
+                n_s += 1;
+                tc_fence_after_sync();
+                // the row in four pieces of 32 columns, from tensor memory twice (all 128 at once do not fit the registers)
+                const int rows = x.n_rows - (x.t0 + t) * kShTile;
+                uint32_t s[2][32];
+                float mx = -INFINITY;
+                tmem_ld_x32(ts, s[0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    tmem_wait_ld();
+                    reg_fence32(s[j & 1]);
+                    if (j < 3) tmem_ld_x32(ts + 32 * (j + 1), s[(j + 1) & 1]);
+                    else tmem_ld_x32(ts, s[0]);                  // the first piece again
+                    if (rows >= 32 * (j + 1)) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(s[j & 1][k]), __uint_as_float(s[j & 1][k + 1])));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (32 * j + k < rows) mx = fmaxf(mx, __uint_as_float(s[j & 1][k]));
+                    }
+                }
+                mx *= p.scale_log2e;
+                if (i == 0) {
+                    m_ref = mx;
+                } else {
+                    const bool grown = mx > m_ref + kShGrow;
+                    if (__any_sync(0xffffffffu, grown)) {
+                        const float m_new = fmaxf(m_ref, mx), f = m_ref == m_new ? 1.0f : fast_ex2(m_ref - m_new);
+                        m_ref = m_new;
+                        l_run *= f;
+#pragma unroll 1
+                        for (int j = 0; j < kD / 32; ++j) {
+                            uint32_t o[32];
+                            tmem_ld_x32(to + 32 * j, o);
+                            tmem_wait_ld();
+                            reg_fence32(s[0]);
+                            reg_fence32(o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st_x32(to + 32 * j, o);
+                        }
+                    }
+                }
+                const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
+                const uint64_t scale2 = f2_pack(p.scale_log2e, p.scale_log2e), minus_m = f2_pack(-m_use, -m_use);
+                uint64_t sum2 = f2_pack(0.0f, 0.0f), sum2b = sum2;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t *v = s[j & 1];
+                    tmem_wait_ld();
+                    reg_fence32(v);
+                    if (j < 3) tmem_ld_x32(ts + 32 * (j + 1), s[(j + 1) & 1]);
+                    if (rows < 32 * (j + 1)) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (32 * j + k >= rows) v[k] = 0xff800000u;
+                    }
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        float a, b, d, e;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale2, minus_m), a, b);
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), scale2, minus_m), d, e);
+                        a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
+                        sum2 = f2_add(sum2, f2_pack(a, b));
+                        sum2b = f2_add(sum2b, f2_pack(d, e));
+                        pk[k / 2] = pack_bf16x2(a, b);           // P: 8 bits, relative to the row's maximum; the sum takes all 24
+                        pk[k / 2 + 1] = pack_bf16x2(d, e);
+                    }
+                    tmem_st_x16(ts + 16 * j, pk);                // over columns that have been read
+                }
+                float a, b;
+                f2_unpack(f2_add(sum2, sum2b), a, b);
+                l_run += a + b;
+                tmem_wait_st();
+                tc_fence_before_sync();
+                mbar_arrive(p_full + 8 * w);
+            }
+            if (ok && !__all_sync(0xffffffffu, mbar_wait(done, n_piece & 1, &abort_s))) ok = false;
+            tc_fence_after_sync();
+            // the groups tell one another their (m, l) where S was
+            uint32_t theirs[2] = {__float_as_uint(m_ref), __float_as_uint(l_run)};
+            tmem_st_x2(ts, theirs);
+            tmem_wait_st();
+            tc_fence_before_sync();
+            named_barrier_sync(1, 256);
+            tc_fence_after_sync();
+            if (abort_s) ok = false;
+            n_piece += 1;
+            if (!ok) {
+                for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
+                continue;
+            }
+            const int qr = two ? w * 128 + row : row;
+            float *out = const_cast<float *>(p.v.part) + (out_row + qr) * kD;
+            const bool store = qr < n_rows_q;
+            if (two) {
+#pragma unroll
+                for (int j = 0; j < kD / 32; ++j) {
+                    uint32_t o[32];
+                    tmem_ld_x32(to + 32 * j, o);
+                    tmem_wait_ld();
+                    reg_fence32(o);
+                    if (store)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) st_global_v8(out + 32 * j + k, reinterpret_cast<const float *>(o + k));
+                }
+                if (store) ml_out[qr] = make_float2(m_ref, l_run);
+            } else {
+                // both groups' parts of the row, half of the columns each
+                tmem_ld_x2(tmem + lanes + 256 * (1 - w), theirs);
+                tmem_wait_ld();
+                asm volatile("" : "+r"(theirs[0]), "+r"(theirs[1])::"memory");
+                const float m_other = __uint_as_float(theirs[0]), l_other = __uint_as_float(theirs[1]);
+                const float m = fmaxf(m_ref, m_other);
+                const float f_mine = m_ref == m ? 1.0f : fast_ex2(m_ref - m), f_theirs = m_other == m ? 1.0f : fast_ex2(m_other - m);
+                const bool both = n > 1;                          // of one tile the second group had nothing
+#pragma unroll
+                for (int j = 0; j < kD / 64; ++j) {
+                    const uint32_t col = w * (kD / 2) + 32 * j;
+                    uint32_t o0[32], o1[32];
+                    tmem_ld_x32(tmem + lanes + 128 + col, o0);
+                    if (both) tmem_ld_x32(tmem + lanes + 384 + col, o1);
+                    tmem_wait_ld();
+                    reg_fence32(o0);
+                    if (both) {
+                        reg_fence32(o1);
+                        const float f0 = w == 0 ? f_mine : f_theirs, f1 = w == 0 ? f_theirs : f_mine;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            o0[k] = __float_as_uint(__uint_as_float(o0[k]) * f0 + __uint_as_float(o1[k]) * f1);
+                    }
+                    if (store)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) st_global_v8(out + col + k, reinterpret_cast<const float *>(o0 + k));
+                }
+                if (store && w == 0)
+                    ml_out[qr] = both ? make_float2(m, l_run * f_mine + l_other * f_theirs) : make_float2(m_ref, l_run);
+            }
+            tc_fence_before_sync();
+            mbar_arrive(o_free);
+        }
+        if (!ok && threadIdx.x % 128 == 0) atomicCAS(p.status, 0, 5 /* KVZAP_ERR_TIMEOUT */);
+    }
+    if (!ok && warp >= 8) {
+        // a wait ran out: the copies already in flight get a fixed time to land
+        if (lane == 0) atomicCAS(p.status, 0, 5 /* KVZAP_ERR_TIMEOUT */);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000LL) { }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace kvzap
