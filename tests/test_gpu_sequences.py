@@ -1,0 +1,506 @@
+"""Whole sequences of the decode cache -- forked, released, packed, unpacked -- against a model of the lists in Python.
+
+Rows are copied bit for bit and the scores are the GPU's own, so everything is compared exactly.  The model appends a token at a
+time by the rule of the decode step: a token that leaves the window joins the prefix iff its score is at least tau.
+"""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_07891_b200 import synth
+
+pytestmark = pytest.mark.gpu
+
+TAU = 0.0
+D_MODEL = 64
+
+
+class Model:
+    """Lists (b, l, h): prefix rows, window of (score, k, v), tokens appended; active slots."""
+
+    def __init__(self, B, L, H, w):
+        self.B, self.L, self.H, self.w = B, L, H, w
+        self.lists = {(b, l, h): ([], [], 0) for b in range(B) for l in range(L) for h in range(H)}
+        self.active = [True] * B
+
+    def append(self, b, l, h, score, k, v):
+        prefix, window, n = self.lists[b, l, h]
+        window.append((score, k, v))
+        if len(window) > self.w:
+            s, k, v = window.pop(0)
+            if s >= TAU:
+                prefix.append((k, v))
+        self.lists[b, l, h] = (prefix, window, n + 1)
+
+    def copy(self, src, dst):
+        for l in range(self.L):
+            for h in range(self.H):
+                prefix, window, n = self.lists[src, l, h]
+                self.lists[dst, l, h] = (list(prefix), list(window), n)
+        self.active[dst] = self.active[src]
+
+    def release(self, b):
+        for l in range(self.L):
+            for h in range(self.H):
+                self.lists[b, l, h] = ([], [], 0)
+        self.active[b] = False
+
+    def packed(self, seqs):
+        K, V, start, tokens, scores = [], [], [0], [], []
+        for b in seqs:
+            for l in range(self.L):
+                for h in range(self.H):
+                    prefix, window, n = self.lists[b, l, h]
+                    rows = prefix + [(k, v) for _, k, v in window]
+                    K += [k for k, _ in rows]
+                    V += [v for _, v in rows]
+                    start.append(start[-1] + len(rows))
+                    tokens.append(n)
+                    scores.append([s for s, _, _ in window] + [0.0] * (self.w - len(window)))
+        return K, V, start, tokens, np.array(scores, dtype=np.float32)
+
+
+class World:
+    """A context with one cache, and the model that follows it."""
+
+    def __init__(self, binding, B, L, H, D, w, page, n_pages, width=None, seed=1):
+        self.binding, self.H, self.L, self.D, self.B, self.page = binding, H, L, D, B, page
+        self.rng = np.random.default_rng(seed)
+        self.ctx = binding.Kvzap(D_MODEL, 0, H, D, L, max_tokens=max(B, 512), max_seqs=B)
+        for l in range(L):
+            self.ctx.set_weights(l, *[x.cuda() for x in synth.linear_weights(D_MODEL, H, 10 + l, "cpu", 0.3)])
+        self.K_pool = torch.full((n_pages, page, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        self.V_pool = torch.full_like(self.K_pool, float("nan"))
+        self.cache = self.ctx.create_cache(B, w, page, self.K_pool, self.V_pool, width or n_pages)
+        self.model = Model(B, L, H, w)
+
+    def rows(self, *shape):
+        return torch.from_numpy(self.rng.integers(0, 0x7f00, shape + (self.D,)).astype(np.int16)).view(torch.bfloat16)
+
+    def hidden(self, *shape):
+        return torch.from_numpy(self.rng.standard_normal(shape + (D_MODEL,)).astype(np.float32)).bfloat16()
+
+    def step(self):
+        X, K, V = self.hidden(self.L, self.B), self.rows(self.L, self.B, self.H), self.rows(self.L, self.B, self.H)
+        scores = torch.empty(self.L, self.B, self.H, device="cuda")
+        self.cache.decode_step(0, self.L, X.cuda(), K.cuda(), V.cuda(), TAU, scores_out=scores)
+        s, Kb, Vb = scores.cpu().numpy(), synth.bits(K), synth.bits(V)
+        for b in range(self.B):
+            if not self.model.active[b]:
+                continue
+            for l in range(self.L):
+                for h in range(self.H):
+                    self.model.append(b, l, h, s[l, b, h], Kb[l, b, h].tobytes(), Vb[l, b, h].tobytes())
+
+    def prompt(self, b, n):
+        for l in range(self.L):
+            X, K, V = self.hidden(n), self.rows(self.H, n), self.rows(self.H, n)
+            scores = self.cache.prefill(l, b, X.cuda(), K.cuda(), V.cuda(), TAU)
+            s, Kb, Vb = scores.cpu().numpy(), synth.bits(K), synth.bits(V)
+            for h in range(self.H):
+                for t in range(n):
+                    self.model.append(b, l, h, s[t, h], Kb[h, t].tobytes(), Vb[h, t].tobytes())
+        self.model.active[b] = True
+
+    def fork(self, src, dst):
+        self.cache.fork(src, dst)
+        for s, d in zip(src, dst):
+            self.model.copy(s, d)
+
+    def release(self, b):
+        self.cache.release_seq(b)
+        self.model.release(b)
+
+    def check(self, seqs=None):
+        seqs = list(range(self.B)) if seqs is None else seqs
+        K, V, start, tokens, scores = self.cache.pack(seqs)
+        torch.cuda.synchronize()
+        assert self.ctx.poll_status() == 0
+        wK, wV, wstart, wtokens, wscores = self.model.packed(seqs)
+        assert start.tolist() == wstart
+        assert tokens.tolist() == wtokens
+        np.testing.assert_array_equal(scores.cpu().numpy(), wscores.reshape(scores.shape))
+        for got, want in ((K, wK), (V, wV)):
+            assert [r.tobytes() for r in synth.bits(got)] == want
+        lengths = self.cache.lengths()[torch.tensor(seqs)].flatten().tolist()
+        assert lengths == [b - a for a, b in zip(wstart, wstart[1:])]
+
+    def tables(self):
+        """Page numbers of every list, and the allocator's cursor."""
+        n = self.B * self.L * self.H
+        width = self.cache_width()
+        prefix = torch.empty(n, dtype=torch.int32, device="cuda")
+        table = torch.empty(n, width, dtype=torch.int32, device="cuda")
+        cursor = torch.empty(1, dtype=torch.int32, device="cuda")
+        self.binding.kvzap_cache_snapshot(self.ctx.handle, self.cache.handle, prefix, table, cursor)
+        p, t = prefix.cpu().numpy(), table.cpu().numpy()
+        return [t[i, :-(-p[i] // self.page)].tolist() for i in range(n)], p, int(cursor.item())
+
+    def cache_width(self):
+        return self.width if hasattr(self, "width") else self.K_pool.shape[0]
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2601_07891_b200 import binding as b
+    b.load()
+    return b
+
+
+def _pages_are_sound(world):
+    """A partly filled page has one owner, a full one is in as many tables, at the same place, as lists share it."""
+    lists, prefix, cursor = world.tables()
+    owners = {}
+    for i, pages in enumerate(lists):
+        for j, p in enumerate(pages):
+            assert 0 <= p < world.K_pool.shape[0]
+            owners.setdefault(p, []).append((i, j, (j + 1) * world.page <= prefix[i]))
+    for p, who in owners.items():
+        if len(who) > 1:
+            assert all(full for _, _, full in who), "a shared page is not full"
+            assert len({j for _, j, _ in who}) == 1
+            assert len({i for i, _, _ in who}) == len(who)
+    return set(owners), cursor
+
+
+@pytest.mark.parametrize("D,w,page,L,H,steps", [
+    (128, 16, 16, 2, 8, 70),
+    (64, 0, 16, 1, 2, 40),       # no window
+    (72, 5, 7, 2, 3, 61),        # 8-bit rows, pages of an odd size
+    (8, 3, 1, 1, 1, 30),         # one row a page: never a partly filled one
+    (128, 32, 128, 1, 8, 20),    # everything still in the window: nothing to share
+])
+def test_children_go_on_by_themselves(binding, D, w, page, L, H, steps):
+    world = World(binding, 5, L, H, D, w, page, 400, seed=steps)
+    for _ in range(steps):
+        world.step()
+    world.fork([0, 0, 1], [2, 4, 3])
+    world.check()
+    _pages_are_sound(world)
+    for _ in range(2 * page % 41 + 3):
+        world.step()
+    world.check()
+    world.fork([4], [0])                                   # a child becomes the source of its own source's slot
+    world.prompt(0, 40)
+    world.check()
+    _pages_are_sound(world)
+    world.check([3])
+    world.check([4, 0])
+
+
+def test_released_pages_wait_for_their_last_owner(binding):
+    """Whatever the order in which owners go, every page comes back once: the pool is taken up in full afterwards."""
+    for order in ([0, 1, 2, 3], [3, 2, 1, 0], [1, 3, 0, 2]):
+        world = World(binding, 4, 1, 2, 8, 4, 4, 64, seed=7)
+        world.release(1)
+        world.release(2)
+        world.release(3)
+        world.prompt(0, 60)
+        world.fork([0, 0], [1, 2])
+        world.step()
+        world.fork([2], [3])
+        world.step()
+        world.check()
+        for b in order[:2]:
+            world.release(b)
+            world.check()
+            _pages_are_sound(world)
+        for b in order[2:]:
+            world.release(b)
+        # sequences of 31 pages a list in two slots: 124 lists' pages are more than a pool with a page lost could give
+        rows = 32 * 4
+        start = torch.arange(0, 3, dtype=torch.int64, device="cuda") * rows
+        K = world.rows(2 * rows).cuda()
+        tokens = torch.zeros(2, dtype=torch.int32, device="cuda")
+        scores = torch.zeros(2, 4, device="cuda")
+        world.cache.unpack([1], K, K, start, tokens, scores)
+        torch.cuda.synchronize()
+        assert world.ctx.poll_status() == 0                 # 64 pages, all of them
+        used, _ = _pages_are_sound(world)
+        assert used == set(range(64))
+
+
+def test_release_of_several_owners_in_one_call(binding):
+    """A fork over children releases several owners of the same pages at the same time."""
+    world = World(binding, 40, 1, 4, 8, 2, 2, 600, seed=3)
+    world.prompt(0, 90)
+    children = list(range(1, 39))
+    world.fork([0] * len(children), children)
+    world.check()
+    world.prompt(39, 50)
+    world.fork([39] * len(children), children)              # the 38 old children go, slot 0 keeps its pages
+    world.check()
+    used, cursor = _pages_are_sound(world)
+    world.release(0)
+    world.fork([39], [0])
+    world.check()
+    _pages_are_sound(world)
+
+
+def test_more_pairs_than_a_launch_takes(binding):
+    world = World(binding, 600, 1, 1, 8, 2, 2, 900, width=40, seed=5)
+    world.width = 40
+    world.prompt(0, 21)
+    world.prompt(1, 30)
+    world.fork([i % 2 for i in range(2, 600)], list(range(2, 600)))
+    for seqs in (list(range(0, 250)), list(range(250, 500)), list(range(500, 600))):
+        world.check(seqs)
+    _pages_are_sound(world)
+    for b in range(0, 600, 3):
+        world.release(b)
+    world.check(list(range(0, 200)))
+    _pages_are_sound(world)
+
+
+def test_fork_of_slots_without_a_sequence(binding):
+    world = World(binding, 4, 1, 2, 8, 4, 4, 64, seed=11)
+    for _ in range(20):
+        world.step()
+    world.release(2)
+    world.fork([2], [0])                                    # nothing comes of nothing: the slot is as if released
+    world.step()
+    world.check()
+    world.fork([1], [2])
+    world.fork([3, 3], [2, 0])
+    world.step()
+    world.check()
+    world.cache.fork([], [])
+    world.check()
+
+
+def test_fork_without_pages_left_keeps_what_is_whole(binding):
+    H, page, w = 2, 4, 4
+    world = World(binding, 3, 1, H, 8, w, page, 64, seed=13)
+    world.release(1)
+    world.release(2)
+    world.prompt(0, 40)
+    world.release(0)
+    # slot 0: 30 whole pages and two rows in a list, 124 of 128 rows; two pages left for two lists, then none
+    rows = 30 * page + 2 + w
+    K = world.rows(H * rows).cuda()
+    start = torch.arange(0, H + 1, dtype=torch.int64, device="cuda") * rows
+    tokens = torch.full((H,), 99, dtype=torch.int32, device="cuda")
+    scores = torch.rand(H, w, device="cuda")
+    world.cache.unpack([0], K, K, start, tokens, scores)
+    world.cache.fork([0], [1])
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 0
+    world.cache.fork([0], [2])
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 4
+    assert world.ctx.poll_status() == 0
+    assert world.cache.lengths().flatten().tolist() == [rows] * 4 + [rows - 2] * 2
+    K2, _, start2, tokens2, scores2 = world.cache.pack([2])
+    for h in range(H):
+        want = torch.cat([K[h * rows:h * rows + 30 * page], K[(h + 1) * rows - w:(h + 1) * rows]])
+        assert torch.equal(K2[start2[h]:start2[h + 1]].view(torch.int16), want.view(torch.int16))
+    assert tokens2.tolist() == [99, 99] and torch.equal(scores2, scores)
+    world.cache.release_seq(1)
+    world.cache.fork([0], [2])                              # over the cut one: its pages are counted right
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 0
+    assert world.cache.lengths().flatten().tolist() == [rows] * 2 + [0] * 2 + [rows] * 2
+
+
+@pytest.mark.parametrize("D,w,page,page2,L,H", [(128, 16, 16, 32, 2, 8), (72, 5, 7, 3, 2, 3), (64, 0, 16, 16, 1, 2), (8, 20, 4, 1, 1, 1)])
+def test_packed_sequences_go_on_elsewhere(binding, D, w, page, page2, L, H):
+    """Packed, unpacked into other slots of another cache with other pages: the same lists, and the same ones after more tokens."""
+    world = World(binding, 3, L, H, D, w, page, 300, seed=17)
+    for _ in range(37):
+        world.step()
+    world.prompt(1, 77)
+    packed = world.cache.pack([2, 1])
+    there = World(binding, 4, L, H, D, w, page2, 900, seed=18)
+    there.prompt(3, 30)                                     # what the slot holds goes
+    there.cache.unpack([3, 0], *packed)
+    for slot, b in ((3, 2), (0, 1)):
+        for l in range(L):
+            for h in range(H):
+                prefix, window, n = world.model.lists[b, l, h]
+                there.model.lists[slot, l, h] = (list(prefix), list(window), n)
+    there.check()
+    _pages_are_sound(there)
+    for _ in range(w + 9):
+        there.step()
+    there.check()
+    _pages_are_sound(there)
+
+
+def test_pack_matches_the_export_of_each_list(binding):
+    world = World(binding, 2, 2, 3, 24, 6, 5, 200, seed=19)
+    for _ in range(50):
+        world.step()
+    K, V, start, tokens, scores = world.cache.pack([1, 0])
+    for i, (b, l, h) in enumerate((b, l, h) for b in (1, 0) for l in range(2) for h in range(3)):
+        n = int(start[i + 1] - start[i])
+        Ke, Ve = torch.zeros(n, 24, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, 24, dtype=torch.bfloat16, device="cuda")
+        rows = torch.zeros(1, dtype=torch.int32, device="cuda")
+        binding.kvzap_cache_export(world.ctx.handle, world.cache.handle, b, l, h, Ke, Ve, rows)
+        assert int(rows) == n
+        assert torch.equal(K[start[i]:start[i + 1]].view(torch.int16), Ke.view(torch.int16))
+        assert torch.equal(V[start[i]:start[i + 1]].view(torch.int16), Ve.view(torch.int16))
+
+
+def test_pack_into_fewer_rows_leaves_the_rest(binding):
+    world = World(binding, 1, 1, 2, 128, 16, 16, 100, seed=23)
+    world.prompt(0, 300)
+    K, V, start, tokens, scores = world.cache.pack([0])
+    n = K.shape[0]
+    for m in (n - 1, n // 2 + 3, 1, 0):
+        buf = torch.full((2, n + 8, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+        got = world.cache.pack([0], K_out=buf[0, :m], V_out=buf[1, :m])
+        assert torch.equal(got[2], start)
+        for x, want in ((buf[0], K), (buf[1], V)):
+            assert torch.equal(x[:m].view(torch.int16), want[:m].view(torch.int16))
+            assert bool((x[m:] == 3.0).all())
+
+
+def test_unpack_of_too_many_rows_and_of_nonsense(binding):
+    """Rows that find no page are dropped from the prefix's end; starts that do not ascend read nothing they should not."""
+    H, w, page = 2, 4, 4
+    world = World(binding, 2, 1, H, 8, w, page, 16, width=5, seed=29)
+    world.width = 5
+    K = world.rows(200).cuda()
+    tokens = torch.full((H,), 50, dtype=torch.int32, device="cuda")
+    scores = torch.rand(H, w, device="cuda")
+    rows = 7 * page + 1 + w                                # eight pages, a table of five
+    start = torch.arange(0, H + 1, dtype=torch.int64, device="cuda") * rows
+    world.cache.unpack([0], K, K, start, tokens, scores)
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 4
+    got = world.cache.pack([0])
+    assert (got[2][1:] - got[2][:-1]).tolist() == [5 * page + w] * 2
+    for h in range(H):
+        want = torch.cat([K[h * rows:h * rows + 5 * page], K[(h + 1) * rows - w:(h + 1) * rows]])
+        assert torch.equal(got[0][got[2][h]:got[2][h + 1]].view(torch.int16), want.view(torch.int16))
+    _pages_are_sound(world)
+    for bad in ([0, 60, 30], [20, 10, 400], [-50, -20, 9], [5, 5, 5], [0, 1 << 40, 1 << 41]):
+        world.cache.unpack([1], K, K, torch.tensor(bad, dtype=torch.int64, device="cuda"), tokens, scores)
+        torch.cuda.synchronize()
+        world.ctx.poll_status()
+        _pages_are_sound(world)
+        n = world.cache.lengths()[1].flatten().tolist()
+        assert all(0 <= x <= 5 * page + w for x in n)
+    few = torch.tensor([0, 3, 3], dtype=torch.int64, device="cuda")       # fewer rows than a window: that many tokens
+    world.cache.unpack([1], K, K, few, tokens, scores)
+    got = world.cache.pack([1])
+    assert got[3].tolist() == [3, 0] and got[2].tolist() == [0, 3, 3]
+    assert torch.equal(got[0][:3].view(torch.int16), K[:3].view(torch.int16))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_any_order_of_operations(binding, seed):
+    rng = random.Random(seed)
+    w, page = rng.choice([(0, 4), (3, 1), (8, 4), (16, 16)])
+    world = World(binding, 6, rng.choice([1, 2]), rng.choice([1, 3, 8]), rng.choice([8, 72, 128]), w, page, 1500, width=160, seed=seed)
+    world.width = 160
+    for _ in range(25):
+        op = rng.choice(["step", "step", "prompt", "fork", "fork", "release", "move"])
+        if op == "step":
+            for _ in range(rng.randint(1, 12)):
+                world.step()
+        elif op == "prompt":
+            world.prompt(rng.randrange(6), rng.choice([1, 7, 40, 129]))
+        elif op == "fork":
+            slots = rng.sample(range(6), rng.randint(2, 6))
+            cut = rng.randint(1, len(slots) - 1)
+            world.fork([rng.choice(slots[:cut]) for _ in slots[cut:]], slots[cut:])
+        elif op == "release":
+            world.release(rng.randrange(6))
+        else:
+            slots = rng.sample(range(6), rng.randint(1, 3))
+            packed = world.cache.pack(slots)
+            to = rng.sample(range(6), len(slots))
+            lists = {(d, l, h): world.model.lists[s, l, h] for s, d in zip(slots, to) for l in range(world.L) for h in range(world.H)}
+            world.cache.unpack(to, *packed)
+            for key, (prefix, window, n) in lists.items():
+                world.model.lists[key] = (list(prefix), list(window), n)
+            for d in to:
+                world.model.active[d] = True
+        world.check()
+        _pages_are_sound(world)
+
+
+def test_imported_tables_with_shared_pages(binding):
+    """Owners are counted by an import too: a page in two tables comes back when both lists are gone."""
+    world = World(binding, 3, 1, 1, 8, 0, 4, 12, seed=31)
+    prefix = torch.tensor([12, 10, 0], dtype=torch.int32, device="cuda")
+    table = torch.zeros(3, 12, dtype=torch.int32, device="cuda")
+    table[0, :3] = torch.tensor([5, 2, 7])
+    table[1, :3] = torch.tensor([5, 2, 1])
+    world.cache.import_prefix(prefix, table, 8)
+    K = world.rows(6 * 4).cuda()
+    start = torch.tensor([0, 24], dtype=torch.int64, device="cuda")
+    none, zero = torch.zeros(1, 0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    world.cache.release_seq(0)                              # page 7 comes back
+    world.cache.unpack([2], K[:20], K[:20], start.clamp(max=20), zero, none)
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 0                     # 4 fresh ones and that
+    lists, _, _ = world.tables()
+    assert set(lists[2]) == {7, 8, 9, 10, 11} and lists[1] == [5, 2, 1]
+    world.cache.release_seq(1)
+    world.cache.unpack([0], K[:12], K[:12], start.clamp(max=12), zero, none)
+    torch.cuda.synchronize()
+    assert world.ctx.poll_status() == 0
+    assert set(world.tables()[0][0]) == {5, 2, 1}
+
+
+def test_refusals(binding):
+    world = World(binding, 4, 1, 2, 8, 4, 4, 64, seed=37)
+    world.prompt(0, 20)
+    cache, h = world.cache, world.ctx.handle
+
+    def refused(call, status, word):
+        with pytest.raises(binding.KvzapError) as e:
+            call()
+        assert e.value.status == status and word in str(e.value)
+
+    refused(lambda: cache.fork([0], [4]), 1, "out of range")
+    refused(lambda: cache.fork([-1], [1]), 1, "out of range")
+    refused(lambda: cache.fork([0, 0], [1, 1]), 1, "twice")
+    refused(lambda: cache.fork([0], [0]), 1, "both")
+    refused(lambda: cache.fork([0, 1], [1, 2]), 1, "both")
+    with pytest.raises(ValueError):
+        cache.fork([0], [1, 2])
+    K = torch.empty(9, 8, dtype=torch.bfloat16, device="cuda")
+    start, tokens = torch.empty(3, dtype=torch.int64, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    scores = torch.empty(2, 4, device="cuda")
+    for seqs, word in (([4], "out of range"),):
+        refused(lambda: binding.kvzap_cache_pack(h, cache.handle, seqs, K, K, start, tokens, scores), 1, word)
+        refused(lambda: binding.kvzap_cache_unpack(h, cache.handle, seqs, K, K, start, tokens, scores), 1, word)
+    refused(lambda: binding.kvzap_cache_unpack(h, cache.handle, [1, 1], K, K, start, tokens, scores), 1, "twice")
+    refused(lambda: binding.kvzap_cache_unpack(h, cache.handle, [1], K, K, start, tokens, None), 1, "scores")
+    refused(lambda: binding.kvzap_cache_pack(h, cache.handle, [], K, K, start, tokens, None), 1, "n >= 1")
+    lib = binding.load()
+    odd = K.data_ptr() + 2
+    assert lib.kvzap_cache_pack(cache.handle, binding._ints([0]), 1, odd, odd, 4, start.data_ptr(), tokens.data_ptr(), None, None) == 1
+    assert lib.kvzap_cache_fork(cache.handle, None, None, 1, None) == 1
+    assert lib.kvzap_cache_fork(cache.handle, None, None, -1, None) == 1
+    for args in ((K[:, :4], K, start, tokens, scores), (K, K, start[:2], tokens, scores), (K, K, start, tokens.float(), scores),
+                 (K, K, start, tokens, scores[:1])):
+        with pytest.raises(ValueError):
+            cache.unpack([1], *args)
+    world.check()                                           # nothing of all that did anything
+
+
+def test_packing_beside_another_stream_and_in_turns(binding):
+    """Calls one after the other on a stream of their own, without waiting, see one another's results."""
+    world = World(binding, 4, 2, 8, 128, 16, 16, 600, seed=41)
+    for b in range(2):
+        world.prompt(b, 150)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for _ in range(5):
+            world.fork([0, 1], [2, 3])
+            packed = world.cache.pack([2, 3], K_out=torch.empty(5000, 128, dtype=torch.bfloat16, device="cuda"))
+            world.cache.unpack([1, 0], *packed)
+            a = {k: v for k, v in world.model.lists.items() if k[0] >= 2}
+            for (b, l, h), (p, q, n) in a.items():
+                world.model.lists[3 - b, l, h] = (list(p), list(q), n)
+            world.step()
+    stream.synchronize()
+    with torch.cuda.stream(stream):
+        world.check()
