@@ -1,0 +1,282 @@
+"""Rotary positions against the formula in 64 bits.
+
+Tolerances: the angle is a signed multiple of 2^-31 half turns rounded to fp32, off by at most pi (2^-24 + 2^-31) + |position| f 2^-53;
+sincospif, the magnitude and the two products and their sum add at most 2^-21 (|x1| + |x2|) magnitude altogether (sincospif within 2 ulp: 2^-22 each;
+three roundings of 2^-24 each).  bf16: one rounding, half a step, 2^-8 of the value.  8-bit rows: half a step of a code, 2^-4 of
+the value, or 2^-10 scales below the smallest normal code.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2601_07891_b200 import binding as b
+    b.load()
+    return b
+
+
+@pytest.fixture(scope="module")
+def ctx(binding):
+    return binding.Kvzap(64, 0, 8, 128, 1, max_tokens=64)
+
+
+def _frequencies(R, base=10000.0, factor=1.0, original_context=0.0, low=1.0, high=4.0, inv_freq=None):
+    out = []
+    for i in range(R // 2):
+        f = base ** (-2.0 * i / R) if inv_freq is None else inv_freq[i]
+        keep = 0.0
+        if original_context:
+            keep = min(1.0, max(0.0, (original_context * f / (2 * math.pi) - low) / (high - low)))
+        out.append(f * (keep + (1 - keep) / factor))
+    return torch.tensor(out, dtype=torch.float64)
+
+
+def _want(x, positions, freq, R, interleaved, magnitude=1.0, inverse=False):
+    """(rotated, |x1| + |x2| of each element's pair) in 64 bits."""
+    x = x.double().cpu()
+    angle = positions.cpu().double()[:, None] * freq
+    cos, sin = angle.cos()[:, None] * magnitude, angle.sin()[:, None] * magnitude * (-1.0 if inverse else 1.0)
+    y, size = x.clone(), x.abs()
+    a, b = (slice(0, R, 2), slice(1, R, 2)) if interleaved else (slice(0, R // 2), slice(R // 2, R))
+    y[..., a] = x[..., a] * cos - x[..., b] * sin
+    y[..., b] = x[..., b] * cos + x[..., a] * sin
+    size[..., a] = size[..., b] = x[..., a].abs() + x[..., b].abs()
+    return y, size * magnitude
+
+
+def _slack(positions, freq):
+    """What 53 bits leave of an angle, on both sides."""
+    return (positions.cpu().double().abs().max() * freq.max() * 2.0 ** -51).item() if positions.numel() else 0.0
+
+
+def _check(got, want, size, R, slack):
+    err = (got.double().cpu() - want).abs()
+    tol = want.abs() * 2.0 ** -8 + size * (2.0 ** -21 + slack) + 1e-38
+    tol[..., R:] = 0.0                                     # the others are copied
+    assert bool((err <= tol).all()), float((err - tol).max())
+
+
+@pytest.mark.parametrize("T,heads,D,R,interleaved,top", [
+    (1, 1, 128, 128, False, 100),
+    (8, 40, 128, 128, False, 1 << 20),
+    (777, 5, 128, 64, True, 1 << 31),
+    (777, 5, 128, 64, False, 1 << 31),
+    (130, 3, 64, 16, False, 5000),
+    (130, 3, 64, 64, True, 5000),
+    (33, 7, 96, 48, False, 5000),
+    (33, 7, 256, 256, True, 5000),
+    (33, 2, 512, 512, False, 5000),
+    (40, 3, 128, 20, False, 5000),       # rotary dimensions that are no multiple of 16
+    (40, 3, 72, 2, True, 5000),
+    (40, 3, 72, 72, False, 5000),
+    (3, 2, 8, 8, True, 5000),
+    (3, 2, 1024, 1024, False, 5000),
+    (20011, 9, 64, 64, False, 1 << 17),  # a warp per token
+])
+def test_rotation(ctx, T, heads, D, R, interleaved, top):
+    g = torch.Generator().manual_seed(T + R)
+    x = torch.randn(T, heads, D, generator=g).bfloat16()
+    positions = torch.randint(0, top, (T,), generator=g).to(torch.int32)
+    positions[0] = top - 1 if T > 1 else 0
+    ctx.set_rotary(R, D, interleaved=interleaved)
+    freq = _frequencies(R)
+    for inverse in (False, True):
+        got = ctx.rotary(positions.cuda(), x.cuda(), inverse=inverse)
+        _check(got, *_want(x, positions, freq, R, interleaved, inverse=inverse), R, _slack(positions, freq))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(factor=8.0),
+    dict(base=500000.0, factor=8.0, original_context=8192.0, low=1.0, high=4.0),
+    dict(factor=32.0, original_context=4096.0, low=1.0, high=32.0, magnitude=1.3466),
+    dict(inv_freq=[0.0, 1.0, 6.283185307179586, 0.5, 1e-9, 1234.5678, 3.0, 2.0] * 4),
+    dict(inv_freq=[0.25] * 32, factor=4.0),
+])
+@pytest.mark.parametrize("D", [64, 72])
+def test_scaled_frequencies(ctx, kw, D):
+    R, T = 64, 50
+    x = torch.randn(T, 3, D, generator=torch.Generator().manual_seed(3)).bfloat16()
+    positions = torch.tensor([0, 1, -1, -70000, 131071] * 10, dtype=torch.int32)
+    ctx.set_rotary(R, D, **kw)
+    magnitude = kw.get("magnitude", 1.0)
+    freq = _frequencies(R, **{k: v for k, v in kw.items() if k != "magnitude"})
+    got = ctx.rotary(positions.cuda(), x.cuda())
+    _check(got, *_want(x, positions, freq, R, False, magnitude), R, _slack(positions, freq))
+
+
+def test_inverse_is_the_gradient(ctx):
+    """<g, rotate(x)> has gradient rotate^-1(g): against the formula's autograd, and against differences along random directions."""
+    T, D, R = 20, 64, 64
+    g = torch.Generator().manual_seed(9)
+    x, up, way = (torch.randn(T, 2, D, generator=g).bfloat16() for _ in range(3))
+    positions = torch.randint(0, 9000, (T,), generator=g).to(torch.int32)
+    ctx.set_rotary(R, D, magnitude=1.25)
+    freq = _frequencies(R)
+    leaf = x.double().requires_grad_()
+    angle = positions.double()[:, None, None] * freq
+    y = torch.cat([leaf[..., :32] * angle.cos() - leaf[..., 32:] * angle.sin(), leaf[..., 32:] * angle.cos() + leaf[..., :32] * angle.sin()], -1) * 1.25
+    (y * up.double()).sum().backward()
+    got = ctx.rotary(positions.cuda(), up.cuda(), inverse=True).double().cpu()
+    size = _want(up, positions, freq, R, False, 1.25)[1]
+    assert bool(((got - leaf.grad).abs() <= leaf.grad.abs() * 2.0 ** -8 + size * 2.0 ** -20).all())
+    # the operator is linear: the difference quotient is <up, rotate(way)>, each output rounded by 2^-8 of itself
+    turned = ctx.rotary(positions.cuda(), way.cuda()).double().cpu()
+    quotient = (up.double() * turned).sum()
+    room = 2.0 ** -8 * ((up.double() * turned).abs().sum() + (got * way.double()).abs().sum()) + 1e-6
+    assert abs(float(quotient - (got * way.double()).sum())) <= float(room)
+
+
+@pytest.mark.parametrize("odd", [False, True])
+def test_layouts(ctx, odd):
+    """Columns of a fused projection in, head-major rows out; in place; other rows and columns untouched."""
+    T, H, G, D = 101, 3, 2, 128
+    R = 36 if odd else 64
+    g = torch.Generator().manual_seed(4)
+    width = (H * G + 2 * H) * D + (4 if odd else 24)
+    fused = torch.randn(T + 2, width, generator=g).bfloat16().cuda()
+    before = fused.clone()
+    view = fused[1:T + 1, :(H * G + 2 * H) * D].unflatten(1, (H * G + 2 * H, D))
+    Q, K, V = view[:, :H * G], view[:, H * G:H * G + H], view[:, H * G + H:]
+    positions = torch.randint(0, 5000, (T,), generator=g).to(torch.int32).cuda()
+    ctx.set_rotary(R, D)
+    wants = [_want(t, positions, _frequencies(R), R, False) for t in (Q, K)]
+    out = torch.full((2, H + 1, T + 3, D), 5.0, dtype=torch.bfloat16, device="cuda")
+    K_out, V_out = (o[:H, 2:T + 2].transpose(0, 1) for o in out)
+    V_before = V.clone()
+    q, k, v = ctx.rotary(positions, Q, K, V, Q_out=Q, K_out=K_out, V_out=V_out)
+    assert q.data_ptr() == Q.data_ptr()
+    _check(Q, *wants[0], R, 1e-9)
+    _check(K_out, *wants[1], R, 1e-9)
+    assert torch.equal(V_out, V_before)
+    for o in out:
+        assert bool((o[H] == 5.0).all()) and bool((o[:, :2] == 5.0).all()) and bool((o[:, T + 2:] == 5.0).all())
+    fused[1:T + 1, :H * G * D] = before[1:T + 1, :H * G * D]
+    assert torch.equal(fused, before)
+
+
+def test_one_row_for_all_tokens_and_heads(ctx):
+    """Strides of zero: a broadcast input."""
+    x = torch.randn(1, 1, 128).bfloat16().cuda()
+    positions = torch.arange(50, dtype=torch.int32, device="cuda")
+    ctx.set_rotary(128, 128)
+    got = ctx.rotary(positions, x.expand(50, 3, 128))
+    assert torch.equal(got, ctx.rotary(positions, x.expand(50, 3, 128).contiguous()))
+
+
+@pytest.mark.parametrize("T,D,R,interleaved", [(1, 128, 128, False), (77, 64, 32, True), (5000, 128, 128, False), (5000, 64, 64, False)])
+def test_rows_of_8_bits(ctx, T, D, R, interleaved):
+    H = 3
+    g = torch.Generator().manual_seed(T)
+    K, V = (torch.randn(T, H, D, generator=g).bfloat16() * 10.0 ** torch.randint(-3, 4, (T, H, 1), generator=g) for _ in range(2))
+    K, V = K.bfloat16(), V.bfloat16()
+    V[T // 2] = 0.0
+    Q = torch.randn(T, 4 * H, D, generator=g).bfloat16()
+    positions = torch.randint(0, 100000, (T,), generator=g).to(torch.int32)
+    ctx.set_rotary(R, D, interleaved=interleaved)
+    freq = _frequencies(R)
+    out = torch.full((2, H, T + 1, D + 16), 77, dtype=torch.uint8, device="cuda")
+    K8, V8 = (o[:, :T].transpose(0, 1) for o in out)
+    q, _, _ = ctx.rotary(positions.cuda(), Q.cuda(), K.cuda(), V.cuda(), K_out=K8, V_out=V8)
+    _check(q, *_want(Q, positions, freq, R, interleaved), R, 1e-8)
+    assert bool((out[:, :, T:] == 77).all())
+    for rows, (want, size) in ((K8, _want(K, positions, freq, R, interleaved)), (V8, (V.double(), V.double().abs()))):
+        rows = rows.contiguous().cpu()
+        codes = rows[..., :D].contiguous().view(torch.float8_e4m3fn).double()
+        scale = rows[..., D:D + 4].contiguous().view(torch.float32).double()
+        assert bool((rows[..., D + 4:] == 0).all())
+        top = want.abs().amax(-1, keepdim=True)
+        assert bool(((scale - torch.where(top > 0, top / 448.0, torch.ones_like(top))).abs() <= scale * 2.0 ** -19).all())
+        err = (codes * scale - want).abs()
+        tol = want.abs() * 2.0 ** -4 + scale * 2.0 ** -10 + size * 2.0 ** -20
+        assert bool((err <= tol).all())
+        assert bool((codes.abs() <= 448).all())
+
+
+def test_special_values_stay_in_their_pairs(ctx):
+    """Infinities and NaN reach the elements of their pair and no others; position 0 and frequency 0 leave everything as it is."""
+    x = torch.randn(4, 2, 64, generator=torch.Generator().manual_seed(5)).bfloat16()
+    clean = x.clone()
+    x[1, 0, 3], x[2, 1, 40] = float("inf"), float("nan")
+    positions = torch.tensor([0, 5, 9, 12], dtype=torch.int32)
+    ctx.set_rotary(64, 64)
+    got, want = ctx.rotary(positions.cuda(), x.cuda()).cpu(), ctx.rotary(positions.cuda(), clean.cuda()).cpu()
+    bad = torch.zeros_like(x, dtype=torch.bool)
+    bad[1, 0, [3, 35]] = bad[2, 1, [8, 40]] = True
+    assert torch.equal(got[~bad], want[~bad]) and not bool(torch.isfinite(got[bad]).any())
+    assert torch.equal(got[0], x[0])
+
+
+def test_no_tokens_and_no_heads(ctx):
+    ctx.set_rotary(128, 128)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert ctx.rotary(none, torch.zeros(0, 4, 128, dtype=torch.bfloat16, device="cuda")).shape == (0, 4, 128)
+    some = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert ctx.rotary(some, torch.zeros(3, 0, 128, dtype=torch.bfloat16, device="cuda")).shape == (3, 0, 128)
+
+
+def test_captured_and_replayed(ctx):
+    x = torch.randn(9, 4, 128).bfloat16().cuda()
+    positions = torch.arange(9, dtype=torch.int32, device="cuda") * 1000
+    ctx.set_rotary(128, 128)
+    out = torch.empty_like(x)
+    ctx.rotary(positions, x, Q_out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.rotary(positions, x, Q_out=out)
+    positions += 17
+    x.neg_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, ctx.rotary(positions, x))
+
+
+def test_refusals(binding, ctx):
+    fresh = binding.Kvzap(64, 0, 2, 128, 1, max_tokens=64)
+    x = torch.zeros(4, 2, 128, dtype=torch.bfloat16, device="cuda")
+    positions = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(binding.KvzapError) as e:
+        fresh.rotary(positions, x)
+    assert e.value.status == 6
+    nan, inf = float("nan"), float("inf")
+    for kw, status in ((dict(head_dim=12), 2), (dict(head_dim=1032), 2), (dict(rotary_dim=0), 1), (dict(rotary_dim=130), 1), (dict(rotary_dim=5), 1),
+                       (dict(base=1.0), 1), (dict(base=nan), 1), (dict(factor=0.5), 1), (dict(factor=nan), 1), (dict(original_context=-1.0), 1),
+                       (dict(original_context=10.0, low=4.0, high=4.0), 1), (dict(original_context=inf), 1), (dict(magnitude=0.0), 1),
+                       (dict(magnitude=nan), 1), (dict(inv_freq=[-1.0] * 64), 1), (dict(inv_freq=[nan] * 64), 1)):
+        with pytest.raises(binding.KvzapError) as e:
+            fresh.set_rotary(**{**dict(rotary_dim=128, head_dim=128), **kw})
+        assert e.value.status == status, kw
+    with pytest.raises(ValueError):
+        fresh.set_rotary(128, 128, inv_freq=[1.0])
+    fresh.set_rotary(128, 128)
+    for bad in (lambda: fresh.rotary(positions.long(), x), lambda: fresh.rotary(positions[:3], x), lambda: fresh.rotary(positions, x[..., :64]),
+                lambda: fresh.rotary(positions), lambda: fresh.rotary(positions, x, Q_out=x.float()),
+                lambda: fresh.rotary(positions, x, Q_out=torch.empty(4, 2, 128, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+
+    def status(**kw):
+        row = dict(in_=x.data_ptr(), out=x.data_ptr(), in_token=256, in_head=128, out_token=256, out_head=128, n_heads=2, flags=1)
+        n = kw.pop("n", 1)
+        row.update(kw)
+        r = binding.KvzapRows(*[row[f] for f, _ in binding.KvzapRows._fields_])
+        return binding.load().kvzap_rotary(fresh.handle, positions.data_ptr(), 4, (binding.KvzapRows * 4)(r, r, r, r), n, 0, None)
+
+    other = torch.zeros(4, 2, 144, dtype=torch.uint8, device="cuda").data_ptr()
+    assert status(n=0) == 1 and status(n=4) == 1
+    assert status(n_heads=-1) == 1 and status(flags=4) == 1 and status(in_=None) == 1 and status(out=None) == 1
+    assert status(in_token=-256) == 1 and status(out_head=64) == 1 and status(out_token=0) == 1
+    assert status(out_head=136) == 1                         # in place, but not where it was
+    assert status(in_=x.data_ptr() + 1) == 1
+    assert status(flags=3) == 1                              # 8-bit rows in place
+    assert status(flags=3, out=other + 8, out_token=288, out_head=144) == 1
+    assert status(flags=3, out=other, out_token=296, out_head=144) == 1
+    assert status(flags=3, in_=x.data_ptr() + 2, out=other, out_token=288, out_head=144, n_heads=1) == 2
+    fresh.set_rotary(24, 128)
+    assert status(flags=3, out=other, out_token=288, out_head=144) == 2
+    fresh.set_rotary(64, 72)
+    assert status(flags=3, out=other, out_token=288, out_head=144) == 2
