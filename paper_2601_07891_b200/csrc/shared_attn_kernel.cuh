@@ -553,11 +553,6 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     tmem_wait_ld();
                     reg_fence32(v);
                     if (j < 3) tmem_ld_x32(ts + 32 * (j + 1), s[(j + 1) & 1]);
-                    if (rows < 32 * (j + 1)) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (32 * j + k >= rows) v[k] = 0xff800000u;
-                    }
                     uint32_t pk[16];
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) {
@@ -565,6 +560,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale2, minus_m), a, b);
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), scale2, minus_m), d, e);
                         a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
+                        if (32 * j + k >= rows) a = b = d = e = 0.0f;           // past the list's end (rows is a multiple of 16)
                         sum2 = f2_add(sum2, f2_pack(a, b));
                         sum2b = f2_add(sum2b, f2_pack(d, e));
                         pk[k / 2] = pack_bf16x2(a, b);           // P: 8 bits, relative to the row's maximum; the sum takes all 24

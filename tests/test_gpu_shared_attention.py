@@ -1,0 +1,417 @@
+"""Attention of groups that share a prefix, against softmax attention over each list in 64 bits.
+
+Lists are read back from the cache (packed), so the reference knows nothing of groups or pages.  Tolerance: probabilities are rounded to bf16 (half a
+step, 2^-8 of each) before the second product, which sums them in fp32 as the first does (n 2^-24 of the sums of magnitudes at most, n <= 2^12
+here), exponentials are within 2^-20 of themselves, logits within 128 2^-24 of their sums of magnitudes (below 2^-12 of a logit's size
+here, sizes below 2^4: 2^-8 ... of a tenth of the weight at most), and the output is rounded once, half a step, 2^-8 of itself.  Altogether
+2^-8 |O| + (2^-8 + 2^-10) sum p |v|.
+"""
+import random
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+MINUS_INF = float("-inf")
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2601_07891_b200 import binding as b
+    b.load()
+    return b
+
+
+class Setup:
+    """A cache whose pools hold NaN wherever no list has a row."""
+
+    def __init__(self, binding, B, L, H, D, w, page, width, n_pages=None, seed=0, trusted=False):
+        self.binding, self.B, self.L, self.H, self.D, self.w, self.page = binding, B, L, H, D, w, page
+        self.ctx = binding.Kvzap(64, 0, H, D, L, max_tokens=max(B, 64), trusted_producers=trusted)
+        for l in range(L):
+            self.ctx.set_weights(l, torch.zeros(H, 64, dtype=torch.bfloat16, device="cuda"), None)
+        n_pages = n_pages or B * L * H * width
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.K_pool = torch.full((n_pages, page, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        self.V_pool = torch.full_like(self.K_pool, float("nan"))
+        self.cache = self.ctx.create_cache(B, w, page, self.K_pool, self.V_pool, width)
+        for b in range(B):
+            self.cache.release_seq(b)
+
+    def normal(self, *shape):
+        return torch.empty(*shape, dtype=torch.bfloat16, device="cuda").normal_(generator=self.g)
+
+    def fill(self, b, rows, tokens=0):
+        """A sequence of so many paged rows a list (a number, or one for each list) and the last of `tokens` tokens in the window."""
+        n = self.L * self.H
+        rows = [rows] * n if isinstance(rows, int) else rows
+        n_win = min(tokens, self.w)
+        start = torch.tensor([0] + [r + n_win for r in rows]).cumsum(0).cuda()
+        total = int(start[-1])
+        K = self.normal(total, self.D)
+        V = self.normal(total, self.D)
+        self.cache.unpack([b], K, V, start, torch.full((n,), tokens, dtype=torch.int32, device="cuda"),
+                          torch.zeros(n, self.w, device="cuda"))
+
+    def steps(self, n):
+        hidden = torch.zeros(self.L, self.B, 64, dtype=torch.bfloat16, device="cuda")
+        for _ in range(n):
+            self.cache.decode_step(0, self.L, hidden, self.normal(self.L, self.B, self.H, self.D), self.normal(self.L, self.B, self.H, self.D), MINUS_INF)
+
+    def want(self, Q, scale, layers):
+        """(O, sum p |v|) in 64 bits."""
+        K, V, start, _, _ = self.cache.pack(list(range(self.B)))
+        K, V, start = K.double(), V.double(), start.tolist()
+        G = Q.shape[2] // self.H
+        O = torch.zeros(Q.shape, dtype=torch.float64, device="cuda")
+        A = torch.zeros_like(O)
+        for i, l in enumerate(layers):
+            for b in range(self.B):
+                for h in range(self.H):
+                    j = (b * self.L + l) * self.H + h
+                    if start[j] == start[j + 1]:
+                        continue
+                    k, v = K[start[j]:start[j + 1]], V[start[j]:start[j + 1]]
+                    p = torch.softmax(Q[i, b, h * G:(h + 1) * G].double() @ k.t() * scale, -1)
+                    O[i, b, h * G:(h + 1) * G] = p @ v
+                    A[i, b, h * G:(h + 1) * G] = p @ v.abs()
+        return O, A
+
+    def check(self, n_q_heads, layers=None, scale=None, Q=None, spread=1.0, call=None):
+        layers = list(range(self.L)) if layers is None else layers
+        Q = self.normal(len(layers), self.B, n_q_heads, self.D) * spread if Q is None else Q
+        scale = self.D ** -0.5 if scale is None else scale
+        O = torch.full_like(Q, 7.0)
+        if call is None:
+            self.cache.attention_shared(layers[0], layers[-1] + 1, Q, scale, out=O)
+        else:
+            call(Q, scale, O)
+        torch.cuda.synchronize()
+        assert self.ctx.poll_status() == 0
+        want, A = self.want(Q, scale, layers)
+        err = (O.double() - want).abs()
+        tol = want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10)
+        assert bool(torch.isfinite(O).all())
+        assert bool((err <= tol).all()), float((err - tol).max())
+        return O
+
+
+def _ragged(n, low, high, seed):
+    rng = random.Random(seed)
+    return [rng.randint(low, high) for _ in range(n)]
+
+
+@pytest.mark.parametrize("members,G,D,page,w,low,high,steps", [
+    (2, 4, 128, 16, 16, 128, 400, 3),
+    (2, 1, 64, 16, 0, 100, 700, 0),         # no window, one query head per KV head
+    (3, 8, 128, 48, 48, 1000, 1500, 60),    # pages that end inside a tile
+    (5, 7, 64, 80, 16, 300, 900, 20),       # 35 rows of queries, pages of five times 16
+    (16, 8, 128, 128, 128, 128, 128, 1),    # 128 rows of queries; one whole page, one tile
+    (17, 8, 128, 16, 32, 500, 1100, 40),    # 136 rows: two tiles of them
+    (32, 8, 64, 32, 16, 200, 2000, 5),      # 256
+    (33, 8, 128, 16, 16, 300, 600, 5),      # 264: the group in two parts
+    (70, 4, 64, 256, 16, 256, 1200, 5),     # 280, pages longer than a tile
+    (130, 1, 64, 16, 16, 130, 300, 2),
+    (64, 5, 128, 64, 0, 64, 500, 1),
+])
+def test_one_group(binding, members, G, D, page, w, low, high, steps):
+    H = 3
+    width = high // page + (steps + w) // page + 3
+    s = Setup(binding, members, 2, H, D, w, page, width, n_pages=2 * H * (width + members * (steps // page + 3)), seed=members)
+    s.fill(0, _ragged(2 * H, low, high, members), tokens=5 if w else 0)
+    s.cache.fork([0] * (members - 1), list(range(1, members)))
+    s.steps(steps)
+    s.cache.share([list(range(members))], H * G)
+    s.check(H * G)
+    s.check(H * G, layers=[1], spread=4.0)
+
+
+@pytest.mark.parametrize("rows", [0, 1, 15, 16, 127, 128, 129, 144, 255, 256, 257, 1000])
+def test_lengths_of_the_shared_part(binding, rows):
+    s = Setup(binding, 3, 1, 2, 128, 16, 16, 80, seed=rows)
+    s.fill(0, rows)
+    s.cache.fork([0, 0], [1, 2])
+    s.cache.share([[0, 1, 2]], 8)
+    s.check(8)
+    s.steps(20)
+    s.check(8)
+
+
+def test_long_lists_over_all_ctas(binding):
+    """Few long lists: every list in many pieces, some of them the first and last CTA's alone."""
+    s = Setup(binding, 6, 1, 2, 128, 16, 16, 2200, n_pages=6000, seed=1)
+    s.fill(0, [33000, 4111])
+    s.cache.fork([0] * 5, [1, 2, 3, 4, 5])
+    s.steps(4)
+    s.cache.share([[5, 3, 1, 0, 2, 4]], 8)
+    s.check(8)
+    s.check(8, spread=6.0)                  # a few rows have all the weight
+
+
+def test_groups_of_all_kinds(binding):
+    """Several groups, one of members that share nothing, one of a single member, sequences of no group, empty slots; members in any order;
+    groups that share only a part because one was forked from the middle of another's history."""
+    H, G, L = 4, 4, 3
+    s = Setup(binding, 12, L, H, 128, 32, 16, 90, n_pages=20000, seed=2)
+    for b, low, high in ((0, 200, 900), (4, 300, 310), (7, 10, 40), (9, 500, 900)):
+        s.fill(b, _ragged(L * H, low, high, b), tokens=7)
+    s.cache.fork([0, 0, 4], [1, 2, 5])
+    s.steps(120)
+    s.cache.fork([2], [3])                  # shares more with 2 than 2 does with 0
+    s.steps(50)
+    s.cache.share([[3, 0, 2, 1], [5, 4], [7, 9], [8], [10, 11]], H * G)
+    first = s.check(H * G)
+    s.cache.share([[2, 3], [0, 1], [4, 7, 5]], H * G)
+    second = s.check(H * G)
+    assert first.shape == second.shape
+    s.cache.share([], H * G)
+    s.check(H * G)
+
+
+def test_members_that_go_and_come(binding):
+    """Released, forked into, unpacked into, prefilled: what is read is always what the lists hold, the groups told once."""
+    H, G = 2, 4
+    s = Setup(binding, 6, 1, H, 128, 16, 16, 60, n_pages=2000, seed=3)
+    s.fill(0, 500, tokens=3)
+    s.cache.fork([0] * 4, [1, 2, 3, 4])
+    s.steps(18)
+    s.cache.share([[0, 1, 2, 3, 4]], H * G)
+    s.check(H * G)
+    s.cache.release_seq(0)                  # the first member
+    s.check(H * G)
+    s.fill(0, 321, tokens=20)               # another sequence in its slot
+    s.check(H * G)
+    s.cache.fork([0], [2])
+    s.check(H * G)
+    s.steps(40)
+    s.check(H * G)
+    s.cache.release_seq(1)
+    s.cache.release_seq(3)
+    s.check(H * G)
+    s.cache.release_seq(4)                  # nobody shares any more
+    s.check(H * G)
+    n = 90
+    s.cache.prefill(0, 3, torch.zeros(n, 64, dtype=torch.bfloat16, device="cuda"), s.normal(H, n, 128), s.normal(H, n, 128), MINUS_INF) \
+        if n <= s.ctx.max_tokens else None
+    s.check(H * G)
+    prefix = torch.zeros(6 * H, dtype=torch.int32, device="cuda")
+    s.cache.import_prefix(prefix, torch.zeros(6 * H, 60, dtype=torch.int32, device="cuda"), 0)
+    O = s.cache.attention_shared(0, 1, s.normal(1, 6, H * G, 128))
+    assert bool((O == 0).all())
+
+
+def test_imported_tables_share_where_they_agree(binding):
+    """Only leading pages count: equal pages behind a different one are not shared, pages that differ in one list only end it there."""
+    H, D, page, width = 2, 64, 16, 40
+    s = Setup(binding, 3, 1, H, D, 16, page, width, n_pages=400, seed=4)
+    s.K_pool.normal_(generator=s.g)
+    s.V_pool.normal_(generator=s.g)
+    table = torch.arange(width, dtype=torch.int32, device="cuda").repeat(6, 1).view(3, H, width).clone()
+    table[:, 1] += 100
+    table[1, 0, 20] = 300                   # 20 pages in common for head 0, then equal ones again
+    table[2, 1, 3] = 301                    # 3 pages for head 1: fewer rows than a tile
+    prefix = torch.full((3, H), 35 * page, dtype=torch.int32, device="cuda")
+    s.cache.import_prefix(prefix.view(-1), table.view(-1, width), 350)
+    s.cache.share([[0, 1, 2]], H * 4)
+    s.check(H * 4)
+
+
+def test_equal_to_the_plain_call_without_groups(binding):
+    s = Setup(binding, 3, 1, 2, 128, 16, 16, 40, seed=5)
+    s.fill(0, 300)
+    s.cache.fork([0], [1])
+    Q = s.normal(1, 3, 8, 128)
+    assert torch.equal(s.cache.attention_shared(0, 1, Q), s.cache.attention(0, 1, Q))
+    s.cache.share([[2]], 8)
+    assert torch.equal(s.cache.attention_shared(0, 1, Q), s.cache.attention(0, 1, Q))
+
+
+def test_the_same_bits_every_time(binding):
+    s = Setup(binding, 20, 2, 4, 128, 16, 16, 90, n_pages=6000, seed=6)
+    s.fill(0, _ragged(8, 500, 1200, 6))
+    s.cache.fork([0] * 19, list(range(1, 20)))
+    s.steps(30)
+    s.cache.share([list(range(20))], 32)
+    Q = s.normal(2, 20, 32, 128)
+    first = s.cache.attention_shared(0, 2, Q)
+    for _ in range(20):
+        assert torch.equal(s.cache.attention_shared(0, 2, Q), first)
+
+
+@pytest.mark.parametrize("scale,spread", [(0.0, 1.0), (1e-30, 1.0), (1.0, 3.0), (0.125, 20.0)])
+def test_scales(binding, scale, spread):
+    """Uniform weights; logits in the hundreds, where a row has all the weight and the running maximum jumps.  Large logits are off by more: 2^-17
+    of the sum of magnitudes, which for |q| |k| <= 2^13 scale is up to a sixteenth -- there only rows that win clearly are compared."""
+    s = Setup(binding, 4, 1, 2, 128, 16, 16, 90, seed=7)
+    s.fill(0, 1100)
+    s.cache.fork([0] * 3, [1, 2, 3])
+    s.steps(9)
+    s.cache.share([[0, 1, 2, 3]], 8)
+    if spread * scale < 1.0:
+        s.check(8, scale=scale, spread=spread)
+        return
+    Q = s.normal(1, 4, 8, 128) * spread
+    O = s.cache.attention_shared(0, 1, Q, scale)
+    want, A = s.want(Q, scale, [0])
+    plain = s.cache.attention(0, 1, Q, scale)
+    assert bool(torch.isfinite(O).all())
+    # logits off by e weigh p off by about e: |dO| <= 2 e sum p |v|, e = 128 2^-24 sum |q| |k| scale
+    e = 128 * 2.0 ** -24 * float(Q.double().abs().sum(-1).max()) * 5.0 * scale
+    tol = want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10 + 2 * e)
+    assert bool(((O.double() - want).abs() <= tol).all())
+    assert bool(((O.double() - plain.double()).abs() <= 2 * tol).all())
+
+
+def test_growing_logits(binding):
+    """Rows in ascending order of their logits: the maximum grows in every tile, by more and by less than the step at which O is rescaled."""
+    for grow in (1.0, 9.0, 60.0):
+        s = Setup(binding, 2, 1, 1, 64, 0, 16, 130, seed=8)
+        n = 2048
+        q = torch.zeros(64, device="cuda")
+        q[0] = 8.0
+        K = s.normal(n, 64) * 0.25
+        K[:, 0] = (torch.arange(n, device="cuda") / n * grow).bfloat16()
+        V = s.normal(n, 64)
+        s.cache.unpack([0], K, V, torch.tensor([0, n], device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, 0, device="cuda"))
+        s.cache.fork([0], [1])
+        s.cache.share([[0, 1]], 8)
+        s.check(8, Q=q.bfloat16().expand(1, 2, 8, 64).contiguous(), scale=1.0 / 8.0)
+        s.check(8, Q=(-q).bfloat16().expand(1, 2, 8, 64).contiguous(), scale=1.0 / 8.0)
+
+
+def test_layers_in_turns(binding):
+    """More layers than the slots of one launch hold."""
+    s = Setup(binding, 64, 25, 8, 128, 16, 16, 24, n_pages=25 * 8 * (24 + 64 * 2), seed=9)
+    s.fill(0, _ragged(200, 130, 300, 9))
+    s.cache.fork([0] * 63, list(range(1, 64)))
+    s.steps(2)
+    s.cache.share([list(range(0, 32)), list(range(32, 64))], 64)
+    before = s.ctx.launch_count()
+    s.cache.attention_shared(0, 25, s.normal(25, 64, 64, 128))
+    assert s.ctx.launch_count() - before == 4
+    s.check(64)
+    s.check(64, layers=[5, 6, 7])
+
+
+def test_captured_and_replayed(binding):
+    """Replays follow the cache; groups told after the capture make them read every list by itself."""
+    s = Setup(binding, 5, 1, 2, 128, 16, 16, 60, n_pages=1500, seed=10)
+    s.fill(0, 400)
+    s.cache.fork([0] * 3, [1, 2, 3])
+    s.cache.share([[0, 1, 2, 3]], 8)
+    Q, O = s.normal(1, 5, 8, 128), torch.empty(1, 5, 8, 128, dtype=torch.bfloat16, device="cuda")
+    s.cache.attention_shared(0, 1, Q, out=O)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.cache.attention_shared(0, 1, Q, out=O)
+
+    def replay(q, scale, out):
+        Q.copy_(q)
+        graph.replay()
+        out.copy_(O)
+
+    for change in (lambda: None, lambda: s.steps(25), lambda: s.cache.release_seq(2), lambda: s.fill(2, 290), lambda: s.cache.fork([0], [2]),
+                   lambda: s.cache.share([[0, 1], [2, 3]], 8), lambda: s.cache.share([[0, 1, 2, 3, 4]], 8), lambda: s.cache.share([], 8)):
+        change()
+        s.check(8, call=replay)
+
+
+def test_two_captures_of_one_cache(binding):
+    """Two graphs of different layers share the slots; replayed one after the other, in any order, on any stream in turn."""
+    s = Setup(binding, 4, 2, 2, 128, 16, 16, 60, n_pages=1500, seed=11)
+    s.fill(0, _ragged(4, 300, 700, 11))
+    s.cache.fork([0] * 3, [1, 2, 3])
+    s.cache.share([[0, 1, 2, 3]], 8)
+    Q, O = s.normal(2, 4, 8, 128), torch.empty(2, 4, 8, 128, dtype=torch.bfloat16, device="cuda")
+    s.cache.attention_shared(0, 2, Q, out=O)
+    graphs = []
+    for l in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.cache.attention_shared(l, l + 1, Q[l:l + 1], out=O[l:l + 1])
+        graphs.append(graph)
+    want = O.clone()
+    stream = torch.cuda.Stream()
+    for order in ((0, 1), (1, 0), (1, 1, 0)):
+        O.fill_(3.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for l in order:
+                graphs[l].replay()
+        stream.synchronize()
+        a = (O.double() - want.double()).abs()
+        assert bool((a <= want.double().abs() * 2.0 ** -6 + 2.0 ** -7).all())
+
+
+@pytest.mark.parametrize("trusted", [False, True])
+def test_layer_by_layer_as_a_decoder_calls_it(binding, trusted):
+    """Positions, step and attention of each layer in turn, without a wait between: forked, then decoded beside plain attention over the same lists."""
+    B, L, H, G, D = 6, 3, 8, 4, 128
+    s = Setup(binding, B, L, H, D, 32, 16, 60, n_pages=12000, seed=12, trusted=trusted)
+    s.ctx.set_rotary(128, 128, base=1e6)
+    prompt = 200
+    s.fill(0, _ragged(L * H, 150, 500, 12), tokens=prompt)
+    s.fill(4, 160, tokens=20)
+    s.cache.fork([0, 0, 0], [1, 2, 3])
+    s.cache.share([[0, 1, 2, 3]], H * G)
+    hidden = s.normal(L, B, 64)
+    for t in range(40):
+        positions = torch.full((B,), prompt + t, dtype=torch.int32, device="cuda")
+        fused = s.normal(L, B, H * G + 2 * H, D)
+        last = []
+        for l in range(L):
+            q, k, v = s.ctx.rotary(positions, fused[l, :, :H * G], fused[l, :, H * G:H * G + H], fused[l, :, H * G + H:])
+            s.cache.decode_step(l, l + 1, hidden[l:l + 1], k[None], v[None], MINUS_INF)
+            last.append((q[None], s.cache.attention_shared(l, l + 1, q[None])))
+    torch.cuda.synchronize()
+    assert s.ctx.poll_status() == 0
+    for l, (q, O) in enumerate(last):
+        want, A = s.want(q, D ** -0.5, [l])
+        assert bool(((O.double() - want).abs() <= want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10)).all())
+
+
+def test_another_stream_and_pools_beside_nan(binding):
+    s = Setup(binding, 4, 1, 2, 128, 16, 16, 60, n_pages=1500, seed=13)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        s.fill(0, 333)
+        s.cache.fork([0, 0], [1, 2])
+        s.steps(3)
+        s.cache.share([[0, 1, 2]], 8)
+        s.check(8)
+
+
+def test_refusals(binding):
+    s = Setup(binding, 4, 1, 2, 128, 16, 16, 30, seed=14)
+    s.fill(0, 200)
+    s.cache.fork([0], [1])
+
+    def refused(call, status, word):
+        with pytest.raises(binding.KvzapError) as e:
+            call()
+        assert e.value.status == status and word in str(e.value)
+
+    refused(lambda: s.cache.share([[0, 4]], 8), 1, "out of range")
+    refused(lambda: s.cache.share([[0, 1], [1, 2]], 8), 1, "twice")
+    refused(lambda: s.cache.share([[0, 1]], 7), 2, "n_q_heads")
+    refused(lambda: s.cache.share([[0, 1]], 18), 2, "n_q_heads")
+    refused(lambda: s.cache.share([[0, 1]], 0), 2, "n_q_heads")
+    lib = binding.load()
+    ints = binding._ints
+    for start in ([1, 2], [0, -1], [0, 5], [0, 2, 1]):
+        assert lib.kvzap_cache_share(s.cache.handle, ints(start), ints([0, 1, 2, 3]), len(start) - 1, 8, None) == 1
+    assert lib.kvzap_cache_share(s.cache.handle, None, None, 1, 8, None) == 1
+    assert lib.kvzap_cache_share(s.cache.handle, None, None, -1, 8, None) == 1
+    s.cache.share([[0, 1]], 8)
+    Q = s.normal(1, 4, 8, 128)
+    refused(lambda: s.cache.attention_shared(0, 1, s.normal(1, 4, 4, 128)), 1, "told for 8")
+    refused(lambda: s.cache.attention_shared(0, 2, Q), 1, "layer range")
+    refused(lambda: s.cache.attention_shared(0, 1, Q, scale=-1.0), 1, "scale")
+    refused(lambda: s.cache.attention_shared(0, 1, Q, scale=float("nan")), 1, "scale")
+    assert lib.kvzap_decode_attention_shared(s.ctx.handle, s.cache.handle, 0, 1, None, 8, 1.0, Q.data_ptr(), None) == 1
+    s.check(8)
+    for kw in (dict(D=72, w=16, page=16), dict(D=128, w=8, page=16), dict(D=128, w=16, page=24)):
+        other = Setup(binding, 2, 1, 2, kw["D"], kw["w"], kw["page"], 20)
+        refused(lambda: other.cache.share([[0, 1]], 8), 2, "multiples")
