@@ -822,22 +822,18 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
                       : list >= p.head_lists ? p.tail_unit0 + (list - p.head_lists) * p.tail_parts : list * p.n_parts;
     float *unit = n_parts > 1 ? p.part_scratch + static_cast<int64_t>(unit0 + part) * kUnit : nullptr;
     // kShared: what shared_attn_kernel has left of the list's shared rows, added to four elements of one query head
-    const float *sh_part = nullptr;
-    const float2 *sh_ml = nullptr;
-    int64_t sh_stride = 0;
-    int sh_n = 0;
+    int64_t sh_slot = 0;
+    int sh_row = 0, sh_n = 0;
     if constexpr (kShared) {
         if (n_shared > 0) {
             const int h = list % H, b = (list / H) % B, l = list / (H * B);
             const int unit = (l * p.share.n_subs + __ldcg(p.share.seq_sub + b)) * H + h;
-            const int32_t *tile0 = p.share.tile0 + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
-            const int64_t base = __ldcg(tile0), tiles = __ldcg(tile0 + static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H) - base;
+            const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
+            const int64_t base = __ldcg(&lists[0].x), tiles = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x) - base;
             const int ctas = share_ctas(tiles, p.share.n_ctas);
-            const int c0 = share_owner(tiles, ctas, __ldcg(tile0 + unit) - base), c1 = share_owner(tiles, ctas, __ldcg(tile0 + unit + 1) - base - 1);
-            const int64_t row = static_cast<int64_t>(c0 + unit) * p.share.rows_max + __ldcg(p.share.seq_pos + b) * p.group;
-            sh_part = p.share.part + row * kD;
-            sh_ml = p.share.part_ml + row;
-            sh_stride = p.share.rows_max;
+            const int c0 = share_owner(tiles, ctas, __ldcg(&lists[unit].x) - base), c1 = share_owner(tiles, ctas, __ldcg(&lists[unit + 1].x) - base - 1);
+            sh_slot = c0 + unit;
+            sh_row = __ldcg(p.share.seq_pos + b) * p.group;
             sh_n = c1 - c0 + 1;
         }
     }
@@ -848,10 +844,11 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             float4 nv[kPieces];
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
-                const int64_t at = (i0 + j) * sh_stride + gq;
+                const int64_t slot = sh_slot + i0 + j;
                 const bool in = i0 + j < sh_n;
-                ml[j] = in ? __ldcg(sh_ml + at) : make_float2(-INFINITY, 0.0f);
-                nv[j] = in ? __ldcg(reinterpret_cast<const float4 *>(sh_part + at * kD + d)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                ml[j] = in ? __ldcg(p.share.part_ml + slot * p.share.rows_max + sh_row + gq) : make_float2(-INFINITY, 0.0f);
+                nv[j] = in ? __ldcg(reinterpret_cast<const float4 *>(p.share.part + share_part_at<kD>(slot, p.share.rows_max, sh_row + gq, d)))
+                           : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {

@@ -2538,7 +2538,7 @@ struct kvzap_cache {
     int32_t share_box = 0;               // rows per copy of tm_kshare, tm_vshare; 0: not built
     CUtensorMap tm_kshare, tm_vshare;
     int32_t *share_meta = nullptr;       // [1] stamp, [n_seqs + 1] starts, [n_seqs] members, [n_seqs] group, [n_seqs] place there
-    int32_t *share_tile0 = nullptr;      // [L * n_seqs * H + 1]
+    int4 *share_lists = nullptr;         // [L * n_seqs * H + 1]
     void *share_part = nullptr;          // slots of (m, l), then of outputs
     size_t share_part_bytes = 0;
     int32_t share_layers = 0;            // layers of a launch, as far as the slots go
@@ -2846,7 +2846,7 @@ kvzap_status kvzap_cache_destroy(kvzap_cache *cache)
     cudaFree(cache->v.page_cursor); cudaFree(cache->scores); cudaFree(cache->done);
     cudaFree(cache->v.free_stack); cudaFree(cache->v.free_top); cudaFree(cache->v.active);
     cudaFree(cache->v.before); cudaFree(cache->v.page_refs); cudaFree(cache->v.share_rows);
-    cudaFree(cache->share_meta); cudaFree(cache->share_tile0); cudaFree(cache->share_part);
+    cudaFree(cache->share_meta); cudaFree(cache->share_lists); cudaFree(cache->share_part);
     cudaFree(cache->attn_scratch); cudaFree(cache->attn_arrive);
     delete cache;
     return KVZAP_OK;
@@ -3159,6 +3159,21 @@ kvzap_status kvzap_decode_attention_fp8(kvzap_ctx *ctx, kvzap_cache *cache, int3
 
 namespace kvzap {
 
+// Sequences have left their groups: the others' shared rows are found through one that is still there.
+static kvzap_status share_leaders(kvzap_cache *cache, cudaStream_t stream)
+{
+    kvzap_ctx *ctx = cache->ctx;
+    if (cache->share_subs == 0) return KVZAP_OK;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    make_launch(&cfg, attrs, dim3(static_cast<unsigned>(cache->v.n_layers * cache->share_subs * cache->v.n_heads)), dim3(32), 0, stream,
+                !ctx->profiling, 1);
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share_leader_kernel, cache->v, cache->share_meta + 1 + cache->v.n_seqs + 1, cache->share_subs,
+                                       cache->share_lists));
+    ctx->launches += 1;
+    return KVZAP_OK;
+}
+
 // Releases slots (up to kSlotBatch of them); those that hold nothing are left out.
 static kvzap_status release_slots(kvzap_cache *cache, const int32_t *slots, int n, cudaStream_t stream)
 {
@@ -3175,7 +3190,7 @@ static kvzap_status release_slots(kvzap_cache *cache, const int32_t *slots, int 
     KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, release_seqs_kernel, cache->v, list));
     ctx->launches += 1;
     for (int i = 0; i < m; ++i) cache->empty[list.slot[i]] = 1;
-    return KVZAP_OK;
+    return share_leaders(cache, stream);
 }
 
 // Slots in range; with `distinct`, none of them twice.
@@ -3370,6 +3385,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: n_q_heads must be 1..%d times the number of KV heads", kAttnMaxGroup);
     if ((c.head_dim != 64 && c.head_dim != 128) || v.page_tokens % kAttnTileRows != 0 || v.window % kAttnTileRows != 0)
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: head_dim 64 or 128, page_tokens and window multiples of %d are required", kAttnTileRows);
+    if (v.n_seqs >= 1 << 22) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: more than 2^22 sequences");
     int32_t n_members = 0;
     if (n_groups > 0) {
         if (group_start[0] != 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start begins with 0");
@@ -3413,8 +3429,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
         KVZAP_CUDA(ctx, cudaMalloc(&cache->share_meta, sizeof(int32_t) * meta.size()));
         KVZAP_CUDA(ctx, cudaMemsetAsync(cache->share_meta, 0, sizeof(int32_t), stream));
     }
-    if (!cache->share_tile0)
-        KVZAP_CUDA(ctx, cudaMalloc(&cache->share_tile0, sizeof(int32_t) * (static_cast<size_t>(cache->n_lists) + 1)));
+    if (!cache->share_lists) KVZAP_CUDA(ctx, cudaMalloc(&cache->share_lists, sizeof(int4) * (static_cast<size_t>(cache->n_lists) + 1)));
     KVZAP_CUDA(ctx, cudaMemsetAsync(v.share_rows, 0, sizeof(int32_t) * static_cast<size_t>(cache->n_lists), stream));
     meta[0] = ++cache->share_stamp;
     // from pageable host memory: staged by the driver before the call returns
@@ -3453,8 +3468,8 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attrs[2];
     make_launch(&cfg, attrs, dim3(units), dim3(32), 0, stream, false, 1);
-    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share_count_kernel, v, start, member, static_cast<int>(n_subs), cache->share_tile0));
-    share_scan_kernel<<<1, 1024, 0, stream>>>(cache->share_tile0, static_cast<int>(units));
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share_count_kernel, v, start, member, static_cast<int>(n_subs), cache->share_lists));
+    share_scan_kernel<<<1, 1024, 0, stream>>>(cache->share_lists, static_cast<int>(units));
     KVZAP_CUDA(ctx, cudaGetLastError());
     ctx->launches += 2;
     cache->share_subs = n_subs;
@@ -3483,11 +3498,10 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
     memset(&p, 0, sizeof p);
     const size_t B = static_cast<size_t>(v.n_seqs);
     p.c = v;
-    p.sub_start = cache->share_meta + 1;
-    p.sub_seqs = p.sub_start + B + 1;
+    p.sub_seqs = cache->share_meta + 1 + B + 1;
     p.v.seq_sub = p.sub_seqs + B;
     p.v.seq_pos = p.v.seq_sub + B;
-    p.v.tile0 = cache->share_tile0;
+    p.v.lists = cache->share_lists;
     p.v.n_subs = cache->share_subs;
     p.v.rows_max = cache->share_rows_max;
     p.v.n_ctas = ctx->sm_count;
@@ -3577,6 +3591,8 @@ kvzap_status kvzap_cache_import(kvzap_cache *cache, const int32_t *prefix_len, c
         KVZAP_CUDA(ctx, cudaGetLastError());
     }
     std::fill(cache->empty.begin(), cache->empty.end(), 0);
+    const kvzap_status st = share_leaders(cache, stream);
+    if (st != KVZAP_OK) return st;
     KVZAP_CUDA(ctx, cudaStreamSynchronize(stream));
     return KVZAP_OK;
 }

@@ -16,8 +16,8 @@
 // pieces share (of two pieces one after the other at least one of c and u has grown).  decode_attn_kernel works out from the
 // same numbers which slots a list has.
 //
-// Within a CTA: one warp issues the copies (TMA, 128-byte swizzle, boxes of as many rows as pages allow), one the matrix
-// products (tcgen05: S = Q K^T into tensor memory, O += P V with P from tensor memory), and two groups of four warps do the
+// Within a CTA: three warps issue the copies (TMA, 128-byte swizzle, boxes of as many rows as pages allow: a copy takes its warp 75 cycles, 32
+// of them a tile at pages of 16 rows), one the matrix products (tcgen05: S = Q K^T into tensor memory, O += P V with P from tensor memory), and two groups of four warps do the
 // softmax, a row per thread, each with its own S and O in tensor memory, so that one group's exponentials run beside the
 // other's products.  Up to 128 rows of Q: both groups have the same rows and take every other tile, and are joined at the
 // end of a piece.  Up to 256 rows: each group has its own 128 rows and both take every tile.
@@ -32,14 +32,17 @@
 namespace kvzap {
 
 constexpr int kShTile = 128;                 // shared rows per tile, rows of Q per group of warps
-constexpr int kShThreads = 320;              // 2 x 4 softmax warps, producer, products
+constexpr int kShProducers = 3;              // warps that issue copies
+constexpr int kShThreads = 384;              // 2 x 4 softmax warps, producers, products
 constexpr float kShGrow = 8.0f;              // powers of two by which the maximum may grow before O is rescaled
 
 // What decode_attn_kernel needs to find the slots of a list.
 struct ShareView {
-    const int32_t *tile0;                    // [L][n_subs][H] (+ 1) tiles of shared rows before each list, all layers
+    // [L][n_subs][H] (+ 1), all layers: tiles of shared rows before the list; its shared rows and a list of the cache that has them (0 rows: no member
+    // shares any more); first member << 9 | members
+    const int4 *lists;
     const int32_t *seq_sub, *seq_pos;        // [n_seqs] the group that a sequence is in and its place there
-    const float *part;                       // [slot][rows_max][D] unnormalised outputs
+    const float *part;                       // [slot][2][rows_max][D / 2] unnormalised outputs, see share_part_at
     const float2 *part_ml;                   // [slot][rows_max] (m, l); l < 0: a wait ran out
     int32_t n_subs, rows_max, n_ctas;
     // Groups told after this call was captured have another stamp: the call then reads every list by itself.
@@ -54,9 +57,18 @@ struct SharedAttnParams {
     int32_t box_rows;                        // rows per copy: a power of two, 16..128, that divides the page
     float scale_log2e;
     const uint16_t *q;                       // [n_layers_call][B][H * G][D]
-    const int32_t *sub_start, *sub_seqs;     // members of the groups
+    const int32_t *sub_seqs;                 // members of the groups
     int32_t *status;
 };
+
+// Element d (a multiple of 4) of a row in a slot: the columns in two halves, the rows of a half one after the other (a group of warps leaves half
+// the columns of its rows as one piece of memory), the 16-byte pieces of a row turned by the row, as they are in shared memory.
+template <int kD>
+__device__ __forceinline__ int64_t share_part_at(int64_t slot, int rows_max, int row, int d)
+{
+    const int half = d / (kD / 2), piece = (d % (kD / 2)) / 4;
+    return ((slot * 2 + half) * rows_max + row) * (kD / 2) + ((piece ^ (row & 7)) << 2);
+}
 
 // CTAs that take part in a call of so many tiles, and the first tile of CTA i's run.  A piece leaves as many bytes behind as
 // a tile of 128 rows brings in, so a run is at least kShMinTiles tiles, if that leaves SMs idle too.
@@ -152,20 +164,21 @@ __device__ __forceinline__ uint64_t umma_desc_n_major_sw128(uint32_t smem_addr, 
 }
 constexpr uint32_t kIdescBNMajor = 1u << 16;                   // instruction descriptor: B is N-contiguous
 
-__device__ __forceinline__ void st_global_v8(float *p, const float *v)
+// `bytes` (a multiple of 16) of shared memory to global memory, by one thread; its own copies are read / complete behind the waits
+__device__ __forceinline__ void bulk_store(float *dst, uint32_t smem_src, uint32_t bytes)
 {
-    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
-                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
-                 : "memory");
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(dst), "r"(smem_src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // ---------------------------------------------------------------- what a group shares
 // One warp per (layer, group, head): the number of leading pages that the lists of all its members have in common, by comparing
 // their tables, whole pages only.  Members whose slot holds no sequence are left out.  rows of a member's list that are read
-// with the group go to c.share_rows; tiles to n_tiles.  Fewer rows than a tile are not worth a tile.
+// with the group go to c.share_rows; lists[unit].x is the number of tiles, for now.  Fewer rows than a tile are not worth a tile.
 __global__ void __launch_bounds__(32)
 share_count_kernel(const CacheView c, const int32_t *__restrict__ sub_start, const int32_t *__restrict__ sub_seqs, int n_subs,
-                   int32_t *__restrict__ n_tiles)
+                   int4 *__restrict__ lists)
 {
     griddep_wait();
     const int unit = blockIdx.x, lane = threadIdx.x;
@@ -205,18 +218,40 @@ share_count_kernel(const CacheView c, const int32_t *__restrict__ sub_start, con
     if (rows < kShTile) rows = 0;
     for (int i = lane; i < n_mem; i += 32)
         if (c.active[sub_seqs[m0 + i]] != 0) c.share_rows[list_of(i)] = rows;
-    if (lane == 0) n_tiles[unit] = (rows + kShTile - 1) / kShTile;
+    if (lane == 0)
+        lists[unit] = make_int4((rows + kShTile - 1) / kShTile, rows, rows > 0 ? static_cast<int32_t>(list_of(leader)) : 0, m0 << 9 | n_mem);
 }
 
-// Exclusive running sums of v[0 .. n), in place, the total in v[n].
-__global__ void __launch_bounds__(1024) share_scan_kernel(int32_t *__restrict__ v, int n)
+// Members have left their groups: for each (layer, group, head) a list that still has the shared rows.
+__global__ void __launch_bounds__(32)
+share_leader_kernel(const CacheView c, const int32_t *__restrict__ sub_seqs, int n_subs, int4 *__restrict__ lists)
+{
+    griddep_wait();
+    const int unit = blockIdx.x, lane = threadIdx.x;
+    const int h = unit % c.n_heads, l = unit / (c.n_heads * n_subs);
+    const int m0 = lists[unit].w >> 9, n_mem = lists[unit].w & 511;
+    int32_t rows = 0, leader = 0;
+    for (int i0 = 0; i0 < n_mem && rows == 0; i0 += 32) {
+        const int i = i0 + lane;
+        const int32_t li = i < n_mem ? (sub_seqs[m0 + i] * c.n_layers + l) * c.n_heads + h : 0;
+        const int32_t mine = i < n_mem ? c.share_rows[li] : 0;
+        const uint32_t who = __ballot_sync(0xffffffffu, mine > 0);
+        if (who == 0u) continue;
+        rows = __shfl_sync(0xffffffffu, mine, __ffs(who) - 1);
+        leader = __shfl_sync(0xffffffffu, li, __ffs(who) - 1);
+    }
+    if (lane == 0) { lists[unit].y = rows; lists[unit].z = leader; }
+}
+
+// Exclusive running sums of v[0 .. n).x, in place, the total in v[n].x.
+__global__ void __launch_bounds__(1024) share_scan_kernel(int4 *__restrict__ v, int n)
 {
     __shared__ int32_t warp_s[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t before = 0;
     for (int i0 = 0; i0 < n; i0 += 1024) {
         const int i = i0 + threadIdx.x;
-        const int32_t x = i < n ? v[i] : 0;
+        const int32_t x = i < n ? v[i].x : 0;
         int32_t incl = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -229,88 +264,67 @@ __global__ void __launch_bounds__(1024) share_scan_kernel(int32_t *__restrict__ 
         for (int w = 0; w < warp; ++w) at += warp_s[w];
         int32_t all = before;
         for (int w = 0; w < 32; ++w) all += warp_s[w];
-        if (i < n) v[i] = at + incl - x;
+        if (i < n) v[i].x = at + incl - x;
         before = all;
         __syncthreads();
     }
-    if (threadIdx.x == 0) v[n] = before;
+    if (threadIdx.x == 0) v[n] = make_int4(before, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------- the shared rows
 // A CTA's run of tiles, piece by piece; every warp walks it for itself.
 struct SharePiece {
     int unit;                       // list of the call: (layer - layer0, group, head)
-    int l, s, h;                    // ... layer within the call
     int t0, t1;                     // tiles [t0, t1) of the list
     int m0, n_mem;                  // the group's members
     int32_t n_rows;                 // shared rows of the list, 0: no member shares any more
-    int64_t leader;                 // list of a member that does
+    int32_t leader;                 // list of a member that does
 };
-struct ShareWalk {
-    const SharedAttnParams &p;
-    const int32_t *tile0;           // of the call's first list
-    int64_t base, at, end;          // tile numbers within the call
-    int unit, n_units;
-    __device__ ShareWalk(const SharedAttnParams &p_, int lane) : p(p_)
-    {
-        const int per_layer = p.v.n_subs * p.c.n_heads;
-        n_units = p.n_layers_call * per_layer;
-        tile0 = p.v.tile0 + static_cast<int64_t>(p.layer0) * per_layer;
-        at = end = base = 0;
-        unit = 0;
-        if (*p.v.stamp_now != p.v.stamp) return;
-        base = tile0[0];
-        const int64_t tiles = tile0[n_units] - base;
-        const int ctas = share_ctas(tiles, p.v.n_ctas);
-        if (tiles == 0 || static_cast<int>(blockIdx.x) >= ctas) return;
-        at = share_run(tiles, ctas, blockIdx.x);
-        end = share_run(tiles, ctas, blockIdx.x + 1);
-        // the last list that begins at or before the run: 32 probes a round
-        int lo = 0, hi = n_units;                                   // tile0[lo] - base <= at < tile0[hi] - base
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) / 32;
-            const int probe = lo + lane * step;
-            const bool below = probe < hi && tile0[probe] - base <= at;
-            const int n = __popc(__ballot_sync(0xffffffffu, below));    // the first n probes are (lane 0's always is)
-            const int nlo = lo + (n - 1) * step;
-            hi = min(hi, nlo + step);
-            lo = nlo;
-        }
-        unit = lo;
+struct ShareRun { int64_t at, end, base; int unit; };      // tiles of the call [at, end), the first of list `unit`; tiles ahead of the call
+// Whole CTA; one round trip to memory for up to kShThreads lists.
+__device__ __forceinline__ ShareRun share_my_run(const SharedAttnParams &p)
+{
+    __shared__ int unit_s;
+    const int per_layer = p.v.n_subs * p.c.n_heads, n_units = p.n_layers_call * per_layer;
+    const int4 *lists = p.v.lists + static_cast<int64_t>(p.layer0) * per_layer;
+    const bool grouped = *p.v.stamp_now == p.v.stamp;
+    ShareRun r{0, 0, lists[0].x, 0};
+    const int64_t tiles = grouped ? lists[n_units].x - r.base : 0;
+    const int ctas = share_ctas(tiles, p.v.n_ctas);
+    if (static_cast<int>(blockIdx.x) < ctas) {
+        r.at = share_run(tiles, ctas, blockIdx.x);
+        r.end = share_run(tiles, ctas, blockIdx.x + 1);
     }
-    // Whole warp.  False: the run is over.
-    __device__ bool next(SharePiece &x, int lane)
-    {
-        if (at >= end) return false;
-        while (tile0[unit + 1] - base <= at) ++unit;                // lists without tiles
-        const CacheView &c = p.c;
-        const int64_t first = tile0[unit] - base, last = tile0[unit + 1] - base;
-        x.unit = unit;
-        x.h = unit % c.n_heads;
-        x.s = unit / c.n_heads % p.v.n_subs;
-        x.l = unit / (c.n_heads * p.v.n_subs);
-        x.t0 = static_cast<int>(at - first);
-        x.t1 = static_cast<int>((last < end ? last : end) - first);
-        x.m0 = p.sub_start[x.s];
-        x.n_mem = p.sub_start[x.s + 1] - x.m0;
-        x.n_rows = 0;
-        for (int i0 = 0; i0 < x.n_mem && x.n_rows == 0; i0 += 32) {
-            const int i = i0 + lane;
-            int64_t li = 0;
-            int32_t rows = 0;
-            if (i < x.n_mem) {
-                li = (static_cast<int64_t>(p.sub_seqs[x.m0 + i]) * c.n_layers + p.layer0 + x.l) * c.n_heads + x.h;
-                rows = __ldcg(c.share_rows + li);
-            }
-            const uint32_t who = __ballot_sync(0xffffffffu, rows > 0);
-            if (who == 0u) continue;
-            x.n_rows = __shfl_sync(0xffffffffu, rows, __ffs(who) - 1);
-            x.leader = __shfl_sync(0xffffffffu, li, __ffs(who) - 1);
-        }
-        at = first + x.t1;
-        return true;
+    for (int u = threadIdx.x; u < n_units; u += kShThreads) {
+        const int64_t first = lists[u].x - r.base, last = lists[u + 1].x - r.base;
+        if (first <= r.at && r.at < last) unit_s = u;
     }
-};
+    __syncthreads();
+    if (r.at < r.end) r.unit = unit_s;
+    return r;
+}
+// False: the run is over.
+__device__ __forceinline__ bool share_next(const SharedAttnParams &p, ShareRun &r, SharePiece &x)
+{
+    if (r.at >= r.end) return false;
+    const int4 *lists = p.v.lists + static_cast<int64_t>(p.layer0) * p.v.n_subs * p.c.n_heads;
+    int4 mine = __ldg(lists + r.unit);
+    int32_t next = __ldg(&lists[r.unit + 1].x);
+    while (next - r.base <= r.at) {                             // lists without tiles
+        mine = __ldg(lists + ++r.unit);
+        next = __ldg(&lists[r.unit + 1].x);
+    }
+    const int64_t first = mine.x - r.base, last = next - r.base;
+    x.unit = r.unit;
+    x.t0 = static_cast<int>(r.at - first);
+    x.t1 = static_cast<int>((last < r.end ? last : r.end) - first);
+    x.n_rows = mine.y;
+    x.leader = mine.z;
+    x.m0 = mine.w >> 9;
+    x.n_mem = mine.w & 511;
+    r.at = first + x.t1;
+    return true;
+}
 
 // Ring positions of a piece's operands, in the order of their first use: K0, K1, V0, K2, V1, ..., the last K, V, V.
 __device__ __forceinline__ int sh_k_pos(int t) { return t == 0 ? 0 : 2 * t - 1; }
@@ -334,21 +348,21 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t full = bars, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16,
                    q_full = p_full + 16, done = q_full + 8, o_free = done + 8;
     __shared__ uint32_t tmem_s;
-    __shared__ volatile int abort_s;
+    __shared__ volatile int abort_s, failed_s;         // a wait ran out; in a softmax warp
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kShProducers); mbar_init(empty + 8 * i, 1); }
         for (int w = 0; w < 2; ++w) { mbar_init(s_full + 8 * w, 1); mbar_init(p_full + 8 * w, 128); }
         mbar_init(q_full, 256);
         mbar_init(done, 1);
         mbar_init(o_free, 256);
-        abort_s = 0;
+        abort_s = failed_s = 0;
         fence_mbar_init();
         prefetch_tensormap(&tmap_k);
         prefetch_tensormap(&tmap_v);
     }
-    if (warp == 9) {
+    if (warp == 8 + kShProducers) {
         tmem_alloc(smem_u32(&tmem_s), 512);
         tmem_relinquish();
     }
@@ -360,54 +374,58 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     griddep_wait();
     griddep_launch_dependents();
 
-    ShareWalk walk(p, lane);
+    ShareRun walk = share_my_run(p);
     SharePiece x;
     uint32_t pos0 = 0;                       // ring positions used by the pieces so far
     bool ok = true;
     const CacheView &c = p.c;
 
-    if (warp == 8) {
-        // ---- copies.  Lane i: box i / kHalves of the tile, half i % kHalves of its rows
-        const int n_boxes = kShTile / p.box_rows;
-        const int box = lane / kHalves, half = lane % kHalves;
+    if (warp >= 8 && warp < 8 + kShProducers) {
+        // ---- copies.  A tile is n_boxes x kHalves boxes, numbered with the halves fastest; lane i of producer q has number q + kShProducers i
+        const int n_boxes = kShTile / p.box_rows, mine = warp - 8 + kShProducers * lane;
+        const int box = mine / kHalves, half = mine % kHalves;
         const uint64_t policy = l2_policy_evict_first();
-        while (ok && walk.next(x, lane)) {
+        const uint32_t box_bytes = p.box_rows * 128u;
+        while (ok && share_next(p, walk, x)) {
             if (x.n_rows == 0) continue;
             const int n = x.t1 - x.t0;
-            const int32_t *pages = c.page_table + x.leader * c.max_pages;
-            auto row_of = [&](int t) -> int32_t {                           // of this lane's box in the pools, -1: none
+            const int32_t *pages = c.page_table + static_cast<int64_t>(x.leader) * c.max_pages;
+            // of this lane's box of tile t: its page and its first row there (-1: no such box); the page number is on its way while the tiles
+            // before are copied
+            struct Place { int32_t page, row; };
+            auto place_of = [&](int t) -> Place {
                 const int32_t r = (x.t0 + t) * kShTile + box * p.box_rows;
-                if (t >= n || box >= n_boxes || r >= x.n_rows) return -1;
+                if (t >= n || box >= n_boxes || r >= x.n_rows) return {0, -1};
                 const int32_t page_i = r / c.page_tokens;
-                return __ldcg(pages + page_i) * c.page_tokens + (r - page_i * c.page_tokens);
+                return {__ldcg(pages + page_i), r - page_i * c.page_tokens};
             };
-            auto copy = [&](const CUtensorMap *map, uint32_t pos, int t, int32_t row) {
-                const uint32_t at = pos0 + pos, stage = at % kStages, round = at / kStages;
+            auto copy = [&](const CUtensorMap *map, uint32_t pos, const Place &at) {
+                const uint32_t i = pos0 + pos, stage = i % kStages, round = i / kStages;
                 if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
-                const int rows = min(kShTile, x.n_rows - (x.t0 + t) * kShTile);
-                if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, rows * kD * 2u);
+                const uint32_t who = __ballot_sync(0xffffffffu, at.row >= 0);
+                if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, __popc(who) * box_bytes);
                 __syncwarp();
-                if (row >= 0)
-                    tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * p.box_rows * 128u, map, full + 8 * stage,
-                                half * 64, row, policy);
+                if (at.row >= 0)
+                    tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * box_bytes, map, full + 8 * stage, half * 64,
+                                at.page * c.page_tokens + at.row, policy);
             };
-            int32_t cur = row_of(0), next = row_of(1);
-            copy(&tmap_k, 0, 0, cur);
+            Place cur = place_of(0), next = place_of(1);
+            copy(&tmap_k, 0, cur);
             for (int t = 0; ok && t < n; ++t) {
-                const int32_t after = row_of(t + 2);
-                if (t + 1 < n) copy(&tmap_k, sh_k_pos(t + 1), t + 1, next);
-                if (ok) copy(&tmap_v, sh_v_pos(t, n), t, cur);
+                const Place after = place_of(t + 2);
+                if (t + 1 < n) copy(&tmap_k, sh_k_pos(t + 1), next);
+                if (ok) copy(&tmap_v, sh_v_pos(t, n), cur);
                 cur = next;
                 next = after;
             }
             pos0 += 2 * n;
         }
-    } else if (warp == 9) {
+    } else if (warp == 8 + kShProducers) {
         // ---- matrix products: S of step i + 2 behind P V of step i
         const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
         const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
         uint32_t n_p[2] = {0u, 0u}, n_piece = 0;
-        while (ok && walk.next(x, lane)) {
+        while (ok && share_next(p, walk, x)) {
             if (x.n_rows == 0) continue;
             const int n = x.t1 - x.t0;
             const bool two = x.n_mem * p.group > 128;
@@ -463,7 +481,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
         uint32_t n_s = 0, n_piece = 0;
-        while (walk.next(x, lane)) {
+        while (share_next(p, walk, x)) {
             const int n_rows_q = x.n_mem * p.group;
             const bool two = n_rows_q > 128;
             const int slot = static_cast<int>(blockIdx.x) + x.unit;
@@ -471,26 +489,41 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             float2 *ml_out = const_cast<float2 *>(p.v.part_ml) + out_row;
             if (!ok) {                                            // a wait ran out: the outputs that this piece is part of are zeros
                 for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
-                if (x.n_rows > 0) named_barrier_sync(1, 256);     // one for each piece that is worked on, whoever gave up when
+                if (x.n_rows > 0) {                               // as many as of each piece that is worked on, whoever gave up when
+                    named_barrier_sync(1, 256);
+                    named_barrier_sync(1, 256);
+                }
                 continue;
             }
             if (x.n_rows == 0) continue;
-            // Q: 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros
+            // Q: 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros.  What a group of warps has left there of the
+            // piece before has been copied out.
+            bulk_wait_read();
+            named_barrier_sync(1, 256);
             {
-                constexpr int kUnits = kD / 8;
+                constexpr int kUnits = kD / 8, kBatch = 8;
                 const int first = two ? w * 128 : 0, n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
-#pragma unroll 4
-                for (int i = at; i < 128 * kUnits; i += n_thr) {
-                    const int r = i / kUnits, u = i % kUnits, qr = first + r;
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (qr < n_rows_q) {
-                        const int m = qr / p.group;
-                        const int64_t b = p.sub_seqs[x.m0 + m];
-                        const int64_t head = (static_cast<int64_t>(x.l) * c.n_seqs + b) * c.n_heads * p.group + x.h * p.group + (qr - m * p.group);
-                        v = __ldg(reinterpret_cast<const uint4 *>(p.q + head * kD) + u);
+                const int h = x.unit % c.n_heads, l = x.unit / (c.n_heads * p.v.n_subs);
+                const int64_t heads = static_cast<int64_t>(c.n_heads) * p.group;
+                const uint16_t *q = p.q + (static_cast<int64_t>(l) * c.n_seqs * heads + h * p.group) * kD;
+                uint8_t *tile = smem + (kStages + (two ? w : 0)) * kStageBytes;
+                for (int i0 = at; i0 < 128 * kUnits; i0 += n_thr * kBatch) {
+                    uint4 v[kBatch];
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        const int i = i0 + k * n_thr, qr = first + i / kUnits;
+                        v[k] = make_uint4(0u, 0u, 0u, 0u);
+                        if (i < 128 * kUnits && qr < n_rows_q) {
+                            const int m = qr / p.group;
+                            v[k] = __ldg(reinterpret_cast<const uint4 *>(q + (__ldg(p.sub_seqs + x.m0 + m) * heads + (qr - m * p.group)) * kD) + i % kUnits);
+                        }
                     }
-                    *reinterpret_cast<uint4 *>(smem + kStages * kStageBytes + (two ? w : 0) * kStageBytes + (u >> 3) * kHalfBytes + r * 128 +
-                                               (((u & 7) ^ (r & 7)) << 4)) = v;
+#pragma unroll
+                    for (int k = 0; k < kBatch; ++k) {
+                        const int i = i0 + k * n_thr, r = i / kUnits, u = i % kUnits;
+                        if (i < 128 * kUnits)
+                            *reinterpret_cast<uint4 *>(tile + (u >> 3) * kHalfBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4)) = v[k];
+                    }
                 }
                 fence_proxy_async_smem();
                 mbar_arrive(q_full);
@@ -582,29 +615,49 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             tmem_st_x2(ts, theirs);
             tmem_wait_st();
             tc_fence_before_sync();
+            if (!ok) failed_s = 1;                                // all of them go on, or none (the barriers below)
             named_barrier_sync(1, 256);
             tc_fence_after_sync();
-            if (abort_s) ok = false;
+            if (failed_s) ok = false;
             n_piece += 1;
             if (!ok) {
                 for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
                 continue;
             }
+            // Half the columns of this thread's row, in the group's tile of Q, which nothing reads any more (16-byte pieces turned by the row: no two of a warp
+            // in one bank), then all rows of it as one copy.
             const int qr = two ? w * 128 + row : row;
-            float *out = const_cast<float *>(p.v.part) + (out_row + qr) * kD;
-            const bool store = qr < n_rows_q;
+            uint8_t *mine_s = smem + (kStages + w) * kStageBytes + row * (kD * 2);
+            auto put = [&](int j, const uint32_t *o) {               // columns 32 j .. 32 j + 31 of the half
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    *reinterpret_cast<uint4 *>(mine_s + (((8 * j + k) ^ (row & 7)) << 4)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            };
+            auto copy_out = [&](int half) {
+                fence_proxy_async_smem();
+                named_barrier_sync(2 + w, 128);
+                const int rows = min(128, n_rows_q - (two ? w * 128 : 0));
+                if (threadIdx.x % 128 == 0)
+                    bulk_store(const_cast<float *>(p.v.part) + ((static_cast<int64_t>(slot) * 2 + half) * p.v.rows_max + (two ? w * 128 : 0)) * (kD / 2),
+                               qtile + w * kStageBytes, rows * kD * 2);
+            };
             if (two) {
+                for (int half = 0; half < 2; ++half) {
+                    if (half == 1) {
+                        bulk_wait_read();
+                        named_barrier_sync(2 + w, 128);
+                    }
 #pragma unroll
-                for (int j = 0; j < kD / 32; ++j) {
-                    uint32_t o[32];
-                    tmem_ld_x32(to + 32 * j, o);
-                    tmem_wait_ld();
-                    reg_fence32(o);
-                    if (store)
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8) st_global_v8(out + 32 * j + k, reinterpret_cast<const float *>(o + k));
+                    for (int j = 0; j < kD / 64; ++j) {
+                        uint32_t o[32];
+                        tmem_ld_x32(to + half * (kD / 2) + 32 * j, o);
+                        tmem_wait_ld();
+                        reg_fence32(o);
+                        put(j, o);
+                    }
+                    copy_out(half);
                 }
-                if (store) ml_out[qr] = make_float2(m_ref, l_run);
+                if (qr < n_rows_q) ml_out[qr] = make_float2(m_ref, l_run);
             } else {
                 // both groups' parts of the row, half of the columns each
                 tmem_ld_x2(tmem + lanes + 256 * (1 - w), theirs);
@@ -614,6 +667,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const float m = fmaxf(m_ref, m_other);
                 const float f_mine = m_ref == m ? 1.0f : fast_ex2(m_ref - m), f_theirs = m_other == m ? 1.0f : fast_ex2(m_other - m);
                 const bool both = n > 1;                          // of one tile the second group had nothing
+                const float f0 = w == 0 ? f_mine : f_theirs, f1 = w == 0 ? f_theirs : f_mine;
 #pragma unroll
                 for (int j = 0; j < kD / 64; ++j) {
                     const uint32_t col = w * (kD / 2) + 32 * j;
@@ -624,21 +678,20 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     reg_fence32(o0);
                     if (both) {
                         reg_fence32(o1);
-                        const float f0 = w == 0 ? f_mine : f_theirs, f1 = w == 0 ? f_theirs : f_mine;
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
                             o0[k] = __float_as_uint(__uint_as_float(o0[k]) * f0 + __uint_as_float(o1[k]) * f1);
                     }
-                    if (store)
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8) st_global_v8(out + col + k, reinterpret_cast<const float *>(o0 + k));
+                    put(j, o0);
                 }
-                if (store && w == 0)
+                copy_out(w);
+                if (qr < n_rows_q && w == 0)
                     ml_out[qr] = both ? make_float2(m, l_run * f_mine + l_other * f_theirs) : make_float2(m_ref, l_run);
             }
             tc_fence_before_sync();
             mbar_arrive(o_free);
         }
+        bulk_wait();
         if (!ok && threadIdx.x % 128 == 0) atomicCAS(p.status, 0, 5 /* KVZAP_ERR_TIMEOUT */);
     }
     if (!ok && warp >= 8) {
@@ -650,7 +703,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    if (warp == 9) tmem_dealloc(tmem, 512);
+    if (warp == 8 + kShProducers) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace kvzap
