@@ -114,13 +114,11 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t *r)
         "r"(r[30]), "r"(r[31])
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16])
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8])
 {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_ld_x2(uint32_t taddr, uint32_t (&r)[2])
 {
@@ -326,6 +324,22 @@ __device__ __forceinline__ bool share_next(const SharedAttnParams &p, ShareRun &
     return true;
 }
 
+// Registers of the calling warpgroup from here on.  The block is launched with 384 x 168; 256 x 216 + 128 x 72 is the same.
+constexpr int kShRegsSoftmax = 216, kShRegsOthers = 72;
+static_assert(256 * kShRegsSoftmax + 128 * kShRegsOthers <= kShThreads * 168, "no more than the block has");
+__device__ __forceinline__ void named_barrier_arrive(uint32_t id, uint32_t n_threads)
+{
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n_threads) : "memory");
+}
+template <int kRegs> __device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void regs_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+
+__device__ __forceinline__ uint32_t uniform32(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ uint64_t uniform64(uint64_t v)
+{
+    return static_cast<uint64_t>(uniform32(static_cast<uint32_t>(v >> 32))) << 32 | uniform32(static_cast<uint32_t>(v));
+}
+
 // Ring positions of a piece's operands, in the order of their first use: K0, K1, V0, K2, V1, ..., the last K, V, V.
 __device__ __forceinline__ int sh_k_pos(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int sh_v_pos(int t, int n) { return t + 1 < n ? 2 * t + 2 : 2 * n - 1; }
@@ -346,14 +360,14 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t qtile = ring + kStages * kStageBytes;                    // [2] tiles of Q
     const uint32_t bars = qtile + 2 * kStageBytes;
     const uint32_t full = bars, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16,
-                   q_full = p_full + 16, done = q_full + 8, o_free = done + 8;
+                   q_full = p_full + 32, done = q_full + 8, o_free = done + 8;
     __shared__ uint32_t tmem_s;
     __shared__ volatile int abort_s, failed_s;         // a wait ran out; in a softmax warp
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kShProducers); mbar_init(empty + 8 * i, 1); }
-        for (int w = 0; w < 2; ++w) { mbar_init(s_full + 8 * w, 1); mbar_init(p_full + 8 * w, 128); }
+        for (int w = 0; w < 2; ++w) { mbar_init(s_full + 8 * w, 1); mbar_init(p_full + 16 * w, 128); mbar_init(p_full + 16 * w + 8, 128); }
         mbar_init(q_full, 256);
         mbar_init(done, 1);
         mbar_init(o_free, 256);
@@ -380,7 +394,10 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     bool ok = true;
     const CacheView &c = p.c;
 
-    if (warp >= 8 && warp < 8 + kShProducers) {
+    if (warp >= 8) {
+    regs_fewer<kShRegsOthers>();          // the whole warpgroup, at this one place
+    if (warp < 8 + kShProducers) {
+        named_barrier_sync(4, 256 + 32 * kShProducers);       // the queries' loads are on their way: behind a ring full of rows they took 6 us
         // ---- copies.  A tile is n_boxes x kHalves boxes, numbered with the halves fastest; lane i of producer q has number q + kShProducers i
         const int n_boxes = kShTile / p.box_rows, mine = warp - 8 + kShProducers * lane;
         const int box = mine / kHalves, half = mine % kHalves;
@@ -420,7 +437,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             pos0 += 2 * n;
         }
-    } else if (warp == 8 + kShProducers) {
+    } else {
         // ---- matrix products: S of step i + 2 behind P V of step i
         const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
         const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
@@ -439,12 +456,14 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const uint32_t at = pos0 + sh_k_pos(t), stage = at % kStages;
                 if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s))) { ok = false; return; }
                 tc_fence_after_sync();
-                if (lane == 0) {
-                    const uint32_t qa = qtile + (two ? w : 0) * kStageBytes, kb = ring + stage * kStageBytes;
+                // one value for the warp: what a product needs in uniform registers is worked out there, not for each product
+                const uint64_t qd = uniform64(umma_desc_k_major_sw128(qtile + (two ? w : 0) * kStageBytes)), kd = uniform64(umma_desc_k_major_sw128(ring + stage * kStageBytes));
+                const uint32_t to_s = uniform32(tmem + 256 * w);
+                if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < kD / 16; ++ks) {
-                        const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32u;
-                        umma_bf16(tmem + 256 * w, umma_desc_k_major_sw128(qa + off), umma_desc_k_major_sw128(kb + off), idesc_s, ks > 0);
+                        const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32u) >> 4;
+                        umma_bf16(to_s, qd + off, kd + off, idesc_s, ks > 0);
                     }
                     umma_commit(s_full + 8 * w);
                     if (!two || w == 1) umma_commit(empty + 8 * stage);
@@ -456,31 +475,46 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             for (int i = 0; ok && i < steps; ++i) {
                 const int t = tile_of(i), w = i & 1;
                 const uint32_t at = pos0 + sh_v_pos(t, n), stage = at % kStages;
-                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s) &&
-                                             mbar_wait(p_full + 8 * w, n_p[w] & 1, &abort_s))) { ok = false; break; }
-                n_p[w] += 1;
-                tc_fence_after_sync();
-                const int rows = min(kShTile, x.n_rows - (x.t0 + t) * kShTile);      // a multiple of 16
-                if (lane == 0) {
-                    const uint32_t vb = ring + stage * kStageBytes;
-                    for (int ks = 0; ks < rows / 16; ++ks)
-                        umma_bf16_ts(tmem + 256 * w + 128, tmem + 256 * w + 8 * ks, umma_desc_n_major_sw128(vb + ks * 2048u, kHalfBytes), idesc_o,
-                                     i > 1 || ks > 0);
-                    if (!two || w == 1) umma_commit(empty + 8 * stage);
-                    if (i + 1 == steps) umma_commit(done);
+                const int groups = min(kShTile, x.n_rows - (x.t0 + t) * kShTile) / 16;      // rows of 16
+                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s))) { ok = false; break; }
+                const uint64_t vd = uniform64(umma_desc_n_major_sw128(ring + stage * kStageBytes, kHalfBytes));
+                const uint32_t to_s = uniform32(tmem + 256 * w);
+                const bool full_tile = uniform32(groups) >= 8;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {           // as P comes
+                    if (!__all_sync(0xffffffffu, mbar_wait(p_full + 16 * w + 8 * half, n_p[w] & 1, &abort_s))) { ok = false; break; }
+                    tc_fence_after_sync();
+                    const uint32_t more = uniform32(i > 1 || half > 0);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int ks = 4 * half + k;
+                            if (full_tile || ks < groups)
+                                umma_bf16_ts(to_s + 128, to_s + 8 * ks, vd + ks * (2048u >> 4), idesc_o, k > 0 ? 1u : more);
+                        }
+                        if (half == 1) {
+                            if (!two || w == 1) umma_commit(empty + 8 * stage);
+                            if (i + 1 == steps) umma_commit(done);
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (!ok) break;
+                n_p[w] += 1;
                 if (i + 2 < steps) scores(i + 2);
             }
             pos0 += 2 * n;
             n_piece += 1;
         }
+    }
     } else {
         // ---- softmax: thread = row of Q
+        regs_more<kShRegsSoftmax>();
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
         uint32_t n_s = 0, n_piece = 0;
+        bool told = false;                                        // the producers
         while (share_next(p, walk, x)) {
             const int n_rows_q = x.n_mem * p.group;
             const bool two = n_rows_q > 128;
@@ -518,6 +552,8 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             v[k] = __ldg(reinterpret_cast<const uint4 *>(q + (__ldg(p.sub_seqs + x.m0 + m) * heads + (qr - m * p.group)) * kD) + i % kUnits);
                         }
                     }
+                    if (!told) named_barrier_arrive(4, 256 + 32 * kShProducers);
+                    told = true;
 #pragma unroll
                     for (int k = 0; k < kBatch; ++k) {
                         const int i = i0 + k * n_thr, r = i / kUnits, u = i % kUnits;
@@ -535,26 +571,28 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 if (!__all_sync(0xffffffffu, mbar_wait(s_full + 8 * w, n_s & 1, &abort_s))) { ok = false; break; }
                 n_s += 1;
                 tc_fence_after_sync();
-                // the row in four pieces of 32 columns, from tensor memory twice (all 128 at once do not fit the registers)
                 const int rows = x.n_rows - (x.t0 + t) * kShTile;
-                uint32_t s[2][32];
-                float mx = -INFINITY;
-                tmem_ld_x32(ts, s[0]);
+                uint32_t s[128];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    tmem_wait_ld();
-                    reg_fence32(s[j & 1]);
-                    if (j < 3) tmem_ld_x32(ts + 32 * (j + 1), s[(j + 1) & 1]);
-                    else tmem_ld_x32(ts, s[0]);                  // the first piece again
-                    if (rows >= 32 * (j + 1)) {
+                for (int j = 0; j < 4; ++j) tmem_ld_x32(ts + 32 * j, s + 32 * j);
+                tmem_wait_ld();
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(s[j & 1][k]), __uint_as_float(s[j & 1][k + 1])));
-                    } else {
+                for (int j = 0; j < 4; ++j) reg_fence32(s + 32 * j);
+                if (rows < kShTile) {                            // past the list's end (rows is a multiple of 16)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (32 * j + k < rows) mx = fmaxf(mx, __uint_as_float(s[j & 1][k]));
-                    }
+                    for (int j = 16; j < kShTile; ++j)
+                        if (j / 16 * 16 >= rows) s[j] = 0xff800000u;
                 }
+                float mx4[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mx4[j] = __uint_as_float(s[j]);
+#pragma unroll
+                for (int j = 4; j < kShTile; j += 8) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mx4[k] = fmaxf(mx4[k], j + 4 + k < kShTile ? fmaxf(__uint_as_float(s[j + k]), __uint_as_float(s[j + 4 + k])) : __uint_as_float(s[j + k]));
+                }
+                float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx *= p.scale_log2e;
                 if (i == 0) {
                     m_ref = mx;
@@ -569,7 +607,6 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             uint32_t o[32];
                             tmem_ld_x32(to + 32 * j, o);
                             tmem_wait_ld();
-                            reg_fence32(s[0]);
                             reg_fence32(o);
 #pragma unroll
                             for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
@@ -579,34 +616,37 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
                 const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
                 const uint64_t scale2 = f2_pack(p.scale_log2e, p.scale_log2e), minus_m = f2_pack(-m_use, -m_use);
-                uint64_t sum2 = f2_pack(0.0f, 0.0f), sum2b = sum2;
+                float sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t *v = s[j & 1];
-                    tmem_wait_ld();
-                    reg_fence32(v);
-                    if (j < 3) tmem_ld_x32(ts + 32 * (j + 1), s[(j + 1) & 1]);
-                    uint32_t pk[16];
+                for (int j = 0; j < 8; ++j) {                    // 16 columns at a time
+                    uint32_t pk[8];
+                    uint64_t sum2 = 0, sum2b = 0;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
+                    for (int k = 0; k < 16; k += 4) {
+                        const uint32_t *v = s + 16 * j + k;
                         float a, b, d, e;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale2, minus_m), a, b);
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), scale2, minus_m), d, e);
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, minus_m), a, b);
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, minus_m), d, e);
                         a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
-                        if (32 * j + k >= rows) a = b = d = e = 0.0f;           // past the list's end (rows is a multiple of 16)
-                        sum2 = f2_add(sum2, f2_pack(a, b));
-                        sum2b = f2_add(sum2b, f2_pack(d, e));
+                        sum2 = k == 0 ? f2_pack(a, b) : f2_add(sum2, f2_pack(a, b));
+                        sum2b = k == 0 ? f2_pack(d, e) : f2_add(sum2b, f2_pack(d, e));
                         pk[k / 2] = pack_bf16x2(a, b);           // P: 8 bits, relative to the row's maximum; the sum takes all 24
                         pk[k / 2 + 1] = pack_bf16x2(d, e);
                     }
-                    tmem_st_x16(ts + 16 * j, pk);                // over columns that have been read
+                    float a, b;
+                    f2_unpack(f2_add(sum2, sum2b), a, b);
+                    if (16 * j < rows) sum += a + b;             // past the end: no numbers at a scale of zero, and not read by the product
+                    tmem_st_x8(ts + 8 * j, pk);
+                    if (j == 3) {                                // the product takes the first half while the second is worked out
+                        tmem_wait_st();
+                        tc_fence_before_sync();
+                        mbar_arrive(p_full + 16 * w);
+                    }
                 }
-                float a, b;
-                f2_unpack(f2_add(sum2, sum2b), a, b);
-                l_run += a + b;
+                l_run += sum;
                 tmem_wait_st();
                 tc_fence_before_sync();
-                mbar_arrive(p_full + 8 * w);
+                mbar_arrive(p_full + 16 * w + 8);
             }
             if (ok && !__all_sync(0xffffffffu, mbar_wait(done, n_piece & 1, &abort_s))) ok = false;
             tc_fence_after_sync();
@@ -691,6 +731,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             tc_fence_before_sync();
             mbar_arrive(o_free);
         }
+        if (!told) named_barrier_arrive(4, 256 + 32 * kShProducers);
         bulk_wait();
         if (!ok && threadIdx.x % 128 == 0) atomicCAS(p.status, 0, 5 /* KVZAP_ERR_TIMEOUT */);
     }
