@@ -438,70 +438,72 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             pos0 += 2 * n;
         }
     } else {
-        // ---- matrix products: S of step i + 2 behind P V of step i
+        // ---- matrix products: S of step i + 2 directly behind P V of step i, whose K has been waited for by then: the unit takes 850 cycles for S
+        // (128 bytes of operands a cycle from shared memory) and 640 for P V, and idles through every wait in between
         const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
         const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
         uint32_t n_p[2] = {0u, 0u}, n_piece = 0;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_s));
+            return ok;
+        };
         while (ok && share_next(p, walk, x)) {
             if (x.n_rows == 0) continue;
             const int n = x.t1 - x.t0;
             const bool two = x.n_mem * p.group > 128;
             const int steps = two ? 2 * n : n;
-            if (!__all_sync(0xffffffffu, mbar_wait(q_full, n_piece & 1, &abort_s))) { ok = false; break; }
-            if (n_piece > 0 && !__all_sync(0xffffffffu, mbar_wait(o_free, (n_piece - 1) & 1, &abort_s))) { ok = false; break; }
-            tc_fence_after_sync();
+            if (!wait(q_full, n_piece & 1)) break;
+            if (n_piece > 0 && !wait(o_free, (n_piece - 1) & 1)) break;
             auto tile_of = [&](int i) { return two ? i >> 1 : i; };
-            auto scores = [&](int i) {
-                const int t = tile_of(i), w = i & 1;
-                const uint32_t at = pos0 + sh_k_pos(t), stage = at % kStages;
-                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s))) { ok = false; return; }
-                tc_fence_after_sync();
-                // one value for the warp: what a product needs in uniform registers is worked out there, not for each product
-                const uint64_t qd = uniform64(umma_desc_k_major_sw128(qtile + (two ? w : 0) * kStageBytes)), kd = uniform64(umma_desc_k_major_sw128(ring + stage * kStageBytes));
-                const uint32_t to_s = uniform32(tmem + 256 * w);
-                if (elect_one()) {
+            auto k_at = [&](int i) { return pos0 + sh_k_pos(tile_of(i)); };
+            auto k_full = [&](int i) { return wait(full + 8 * (k_at(i) % kStages), (k_at(i) / kStages) & 1); };
+            const uint64_t qd = uniform64(umma_desc_k_major_sw128(qtile));
+            auto scores = [&](int i) {                            // by one thread
+                const int w = i & 1;
+                const uint32_t stage = k_at(i) % kStages;
+                const uint64_t qw = qd + (two ? w * (kStageBytes >> 4) : 0u), kd = umma_desc_k_major_sw128(ring + stage * kStageBytes);
 #pragma unroll
-                    for (int ks = 0; ks < kD / 16; ++ks) {
-                        const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32u) >> 4;
-                        umma_bf16(to_s, qd + off, kd + off, idesc_s, ks > 0);
-                    }
-                    umma_commit(s_full + 8 * w);
-                    if (!two || w == 1) umma_commit(empty + 8 * stage);
+                for (int ks = 0; ks < kD / 16; ++ks) {
+                    const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32u) >> 4;
+                    umma_bf16(tmem + 256 * w, qw + off, kd + off, idesc_s, ks > 0);
                 }
-                __syncwarp();
+                umma_commit(s_full + 8 * w);
+                if (!two || w == 1) umma_commit(empty + 8 * stage);
             };
-            scores(0);
-            if (ok && steps > 1) scores(1);
+            for (int i = 0; ok && i < min(steps, 2); ++i) {
+                if (!k_full(i)) break;
+                tc_fence_after_sync();
+                if (elect_one()) scores(i);
+                __syncwarp();
+            }
             for (int i = 0; ok && i < steps; ++i) {
                 const int t = tile_of(i), w = i & 1;
                 const uint32_t at = pos0 + sh_v_pos(t, n), stage = at % kStages;
                 const int groups = min(kShTile, x.n_rows - (x.t0 + t) * kShTile) / 16;      // rows of 16
-                if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, (at / kStages) & 1, &abort_s))) { ok = false; break; }
                 const uint64_t vd = uniform64(umma_desc_n_major_sw128(ring + stage * kStageBytes, kHalfBytes));
                 const uint32_t to_s = uniform32(tmem + 256 * w);
-                const bool full_tile = uniform32(groups) >= 8;
+                if (!wait(full + 8 * stage, (at / kStages) & 1)) break;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {           // as P comes
-                    if (!__all_sync(0xffffffffu, mbar_wait(p_full + 16 * w + 8 * half, n_p[w] & 1, &abort_s))) { ok = false; break; }
+                for (int half = 0; half < 2; ++half) {            // as P comes
+                    if (half == 1 && i + 2 < steps && !k_full(i + 2)) break;
+                    if (!wait(p_full + 16 * w + 8 * half, n_p[w] & 1)) break;
                     tc_fence_after_sync();
                     const uint32_t more = uniform32(i > 1 || half > 0);
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int ks = 4 * half + k;
-                            if (full_tile || ks < groups)
-                                umma_bf16_ts(to_s + 128, to_s + 8 * ks, vd + ks * (2048u >> 4), idesc_o, k > 0 ? 1u : more);
+                            if (ks < groups) umma_bf16_ts(to_s + 128, to_s + 8 * ks, vd + ks * (2048u >> 4), idesc_o, k > 0 ? 1u : more);
                         }
                         if (half == 1) {
                             if (!two || w == 1) umma_commit(empty + 8 * stage);
                             if (i + 1 == steps) umma_commit(done);
+                            if (i + 2 < steps) scores(i + 2);
                         }
                     }
                     __syncwarp();
                 }
-                if (!ok) break;
                 n_p[w] += 1;
-                if (i + 2 < steps) scores(i + 2);
             }
             pos0 += 2 * n;
             n_piece += 1;
