@@ -182,6 +182,76 @@ __device__ __forceinline__ int attn_unit(const int32_t *lengths, int n, int n_un
     return __shfl_sync(0xffffffffu, parts, src);
 }
 
+// kShared, more lists than CTAs find room: how long a list's own rows are the host does not know, and what members have added since they were
+// forked is mostly little beside what the lists could hold.  Every list has a CTA; one of more than kAttnLongTiles tiles has as many parts as
+// make that many tiles each, for which a wave of further CTAs stands by at the end of the launch.  If those do not suffice the length of a part is
+// doubled until they do.  Only CTAs of long lists and the further ones look at all lists (some 2 us); the others know by themselves that
+// they are alone.
+constexpr int kAttnLongTiles = 64;
+constexpr int kAttnLongLevels = 24;
+struct AttnLong { int list, part, n_parts, unit0; };       // n_parts 0: nothing to do
+// Whole CTA; tiles_of(i): tiles of list i.  unit < n: the CTA of list `unit`, else a further one.  `tiles` in shared memory, for n lists, or nullptr.
+template <typename F>
+__device__ __forceinline__ AttnLong attn_long(int n, int n_more, int unit, F tiles_of, int32_t *tiles)
+{
+    __shared__ int more_s[kAttnLongLevels], sum_s[2][kAttnWarps], found_s[4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < kAttnLongLevels; i += kAttnThreads) more_s[i] = 0;
+    if (threadIdx.x == 0) found_s[2] = 0;
+    __syncthreads();
+    auto parts_of = [&](int t, int level) { return max(1, static_cast<int>((t + (static_cast<int64_t>(kAttnLongTiles) << level) - 1) / (static_cast<int64_t>(kAttnLongTiles) << level))); };
+    auto get = [&](int i) { return tiles != nullptr ? tiles[i] : tiles_of(i); };
+    constexpr int kBatch = 8;                                   // lists a thread looks up at a time
+    for (int i0 = threadIdx.x; tiles != nullptr && i0 < n; i0 += kAttnThreads * kBatch) {
+        int t[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) t[j] = tiles_of(min(i0 + j * kAttnThreads, n - 1));
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i0 + j * kAttnThreads < n) tiles[i0 + j * kAttnThreads] = t[j];
+    }
+    for (int i = threadIdx.x; i < n; i += kAttnThreads) {
+        const int t = get(i);
+        for (int level = 0; level < kAttnLongLevels && parts_of(t, level) > 1; ++level) atomicAdd(&more_s[level], parts_of(t, level) - 1);
+    }
+    __syncthreads();
+    int level = 0;
+    while (level + 1 < kAttnLongLevels && more_s[level] > n_more) ++level;
+    // this thread's lists -- threadIdx.x, + kAttnThreads, ... -- come one after the other: their further parts, their units
+    int more = 0, units = 0;
+    for (int i = threadIdx.x; i < n; i += kAttnThreads) {
+        const int parts = parts_of(get(i), level);
+        if (parts > 1) { more += parts - 1; units += parts; }
+    }
+    int more_to = more, units_to = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, more_to, o), b = __shfl_up_sync(0xffffffffu, units_to, o);
+        if (lane >= o) { more_to += a; units_to += b; }
+    }
+    if (lane == 31) { sum_s[0][warp] = more_to; sum_s[1][warp] = units_to; }
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) { more_to += sum_s[0][w]; units_to += sum_s[1][w]; }
+    int at = more_to - more, unit0 = units_to - units;
+    const int mine = unit - n;                                  // of the further parts
+    const bool has = unit < n ? unit % kAttnThreads == static_cast<int>(threadIdx.x) : at <= mine && mine < more_to;
+    if (has) {
+        for (int i = threadIdx.x; i < n; i += kAttnThreads) {
+            const int parts = parts_of(get(i), level);
+            if (unit < n ? i == unit : parts > 1 && mine < at + parts - 1) {
+                found_s[0] = i;
+                found_s[1] = unit < n ? 0 : mine - at + 1;
+                found_s[2] = parts;
+                found_s[3] = unit0;
+                break;
+            }
+            if (parts > 1) { at += parts - 1; unit0 += parts; }
+        }
+    }
+    __syncthreads();
+    return {found_s[0], found_s[1], found_s[2], found_s[3]};
+}
+
 constexpr int kAttnTrailerBytes = 16;            // 8-bit rows: fp32 scale + 12 unused bytes behind the codes
 __host__ __device__ constexpr uint32_t attn_stage_bytes(int head_dim, bool fp8 = false)
 {
@@ -267,17 +337,45 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     bool beside = kBeside && static_cast<int>(blockIdx.x) < p.beside_ctas;
     if (!beside && !kShared) griddep_wait();
 
-    int list, part, n_parts = p.n_parts;
+    int list, part, n_parts = p.n_parts, long_unit0 = 0;
     int32_t n_before = 0;                   // kBeside: prefix rows that nothing ahead of this launch still touches
     int32_t n_prefix = 0, n_total = 0;      // rows and tokens now; beside the step not known yet
     const int32_t *before = kBeside ? c.before : c.prefix_len;
     auto cache_list = [&](int i) {          // list i of the call among the cache's lists
         return (static_cast<int64_t>((i / H) % B) * c.n_layers + p.layer0 + i / (H * B)) * H + i % H;
     };
-    const bool grouped = kShared && __ldcg(p.share.stamp_now) == p.share.stamp;
-    auto shared_rows = [&](int i) { return kShared && grouped ? __ldcg(c.share_rows + cache_list(i)) : 0; };
+    const int32_t stamp = kShared ? __ldcg(p.share.stamp_now) : 0;
+    auto shared_rows = [&](int i) {         // the two loads go out together
+        const int32_t rows = kShared ? __ldcg(c.share_rows + cache_list(i)) : 0;
+        return stamp == p.share.stamp ? rows : 0;
+    };
     int32_t n_shared = 0;                   // kShared: of this list
-    if (n_parts > 0) {
+    if (kShared && n_parts > 0) {
+        auto tiles_of = [&](int i) {
+            const int64_t li = cache_list(i);
+            const int32_t rows = __ldcg(c.prefix_len + li), tokens = __ldcg(c.n_tokens + li);
+            return (rows - shared_rows(i) + kAttnTileRows - 1) / kAttnTileRows + (min(tokens, c.window) + kAttnTileRows - 1) / kAttnTileRows;
+        };
+        AttnLong mine{static_cast<int>(blockIdx.x), 0, 1, 0};
+        auto look_up = [&](int i) {
+            n_total = __ldcg(c.n_tokens + cache_list(i));
+            n_prefix = __ldcg(c.prefix_len + cache_list(i));
+            n_shared = shared_rows(i);
+        };
+        if (mine.list < p.extra0) look_up(mine.list);
+        if (mine.list >= p.extra0 || n_prefix - n_shared + min(n_total, c.window) > kAttnLongTiles * kAttnTileRows - 2 * kAttnTileRows) {
+            const bool fits = p.extra0 * 4 <= static_cast<int>(kAttnWarps * kAttnStages * kStageBytes);      // the stages are not in use yet
+            mine = attn_long(p.extra0, static_cast<int>(gridDim.x) - p.extra0, blockIdx.x, tiles_of, fits ? reinterpret_cast<int32_t *>(smem) : nullptr);
+            if (mine.n_parts == 0) return;                         // the whole CTA
+            fence_proxy_async_smem();                              // the copies below write where the lengths were
+            __syncthreads();
+            look_up(mine.list);
+        }
+        list = mine.list;
+        part = mine.part;
+        n_parts = mine.n_parts;
+        long_unit0 = mine.unit0;
+    } else if (n_parts > 0) {
         const int extra = static_cast<int>(blockIdx.x) - p.extra0;
         if (extra < 0) {
             list = static_cast<int>(blockIdx.x) / n_parts;
@@ -291,10 +389,9 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         if (!beside) {
             n_total = __ldcg(c.n_tokens + cache_list(list));
             n_prefix = __ldcg(c.prefix_len + cache_list(list));
-            n_shared = shared_rows(list);
         }
         if (list >= p.head_lists) {
-            const int tiles = ((kBeside ? n_before : n_prefix) - n_shared + min(kBeside ? c.window : n_total, c.window)) / kAttnTileRows;
+            const int tiles = ((kBeside ? n_before : n_prefix) + min(kBeside ? c.window : n_total, c.window)) / kAttnTileRows;
             // as many as the other lists have, or more; a list that is over in 16 tiles has one
             n_parts = tiles < 16 ? 1 : max(n_parts, min(p.tail_parts, tiles / kAttnTailTiles));
             if (part >= n_parts) {                                 // the whole CTA
@@ -561,6 +658,21 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         asm volatile("" ::"r"(seen) : "memory");
         if (lane == 0 && atomicAdd(&queries_s, 1) == kAttnWarps - 1) griddep_launch_dependents();
     };
+    // kShared: the slots of the list's shared rows (looked up while the first rows are on their way)
+    int sh_slot = 0, sh_row = 0, sh_n = 0;
+    auto find_shared = [&]() {
+        if (n_shared > 0) {
+            const int h = list % H, b = (list / H) % B, l = list / (H * B);
+            const int unit = (l * p.share.n_subs + __ldcg(p.share.seq_sub + b)) * H + h;
+            const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
+            const int64_t base = __ldcg(&lists[0].x), tiles = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x) - base;
+            const int ctas = share_ctas(tiles, p.share.n_ctas);
+            const int c0 = share_owner(tiles, ctas, __ldcg(&lists[unit].x) - base), c1 = share_owner(tiles, ctas, __ldcg(&lists[unit + 1].x) - base - 1);
+            sh_slot = c0 + unit;
+            sh_row = __ldcg(p.share.seq_pos + b) * p.group;
+            sh_n = c1 - c0 + 1;
+        }
+    };
     float o[kNTiles][4];
     float m_run = 0.0f, l_run = 0.0f;
     float vref = 0.0f;                     // 8-bit rows: the largest V scale met so far; o is in units of it
@@ -584,6 +696,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     if (again) {
         if (kFp8) take_query();
         if (kBeside && waited) queries_taken();
+        if constexpr (kShared) find_shared();
 #pragma unroll
         for (int i = 0; i < kNTiles; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
         m_run = -INFINITY;
@@ -819,32 +932,18 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     constexpr int kUnit = 16 + kAttnMaxGroup * kD;
     // the list's first unit
     const int unit0 = p.n_parts == 0 ? static_cast<int>(blockIdx.x) - part
+                      : kShared ? long_unit0
                       : list >= p.head_lists ? p.tail_unit0 + (list - p.head_lists) * p.tail_parts : list * p.n_parts;
     float *unit = n_parts > 1 ? p.part_scratch + static_cast<int64_t>(unit0 + part) * kUnit : nullptr;
     // kShared: what shared_attn_kernel has left of the list's shared rows, added to four elements of one query head
-    int64_t sh_slot = 0;
-    int sh_row = 0, sh_n = 0;
-    if constexpr (kShared) {
-        if (n_shared > 0) {
-            const int h = list % H, b = (list / H) % B, l = list / (H * B);
-            const int unit = (l * p.share.n_subs + __ldcg(p.share.seq_sub + b)) * H + h;
-            const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
-            const int64_t base = __ldcg(&lists[0].x), tiles = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x) - base;
-            const int ctas = share_ctas(tiles, p.share.n_ctas);
-            const int c0 = share_owner(tiles, ctas, __ldcg(&lists[unit].x) - base), c1 = share_owner(tiles, ctas, __ldcg(&lists[unit + 1].x) - base - 1);
-            sh_slot = c0 + unit;
-            sh_row = __ldcg(p.share.seq_pos + b) * p.group;
-            sh_n = c1 - c0 + 1;
-        }
-    }
     auto join_shared = [&](int gq, int d, float &m_all, float &den, float4 &num) {
-        constexpr int kPieces = 4;
+        constexpr int kPieces = 6;
         for (int i0 = 0; i0 < sh_n; i0 += kPieces) {
             float2 ml[kPieces];
             float4 nv[kPieces];
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
-                const int64_t slot = sh_slot + i0 + j;
+                const int64_t slot = static_cast<int64_t>(sh_slot) + i0 + j;
                 const bool in = i0 + j < sh_n;
                 ml[j] = in ? __ldcg(p.share.part_ml + slot * p.share.rows_max + sh_row + gq) : make_float2(-INFINITY, 0.0f);
                 nv[j] = in ? __ldcg(reinterpret_cast<const float4 *>(p.share.part + share_part_at<kD>(slot, p.share.rows_max, sh_row + gq, d)))
@@ -899,7 +998,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     // ---- several CTAs per list: the one that arrives last merges all parts, in part order
     __shared__ int last_s;
     __syncthreads();
-    if (threadIdx.x == 0) last_s = arrive_last(p.part_arrive + (list - p.list0), static_cast<uint32_t>(n_parts));
+    if (threadIdx.x == 0) last_s = arrive_last(p.part_arrive + (kShared && p.n_parts > 0 ? long_unit0 : list - p.list0), static_cast<uint32_t>(n_parts));
     __syncthreads();
     if (!last_s) return;
     if constexpr (kShared) griddep_wait();

@@ -3090,6 +3090,9 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
     if (n_lists_call < slots && n_lists_call <= 32 * kAttnListsPerLane) {
         p.n_parts = 0;
         n_ctas = slots;
+    } else if (share) {
+        p.extra0 = static_cast<int32_t>(n_lists_call);          // a CTA per list, and a wave of others for long ones (attn_long)
+        n_ctas = n_lists_call + slots;
     } else {
         const int64_t longest = static_cast<int64_t>(v.max_pages) * v.page_tokens + v.window;
         int64_t parts = static_cast<int64_t>(ctx->sm_count) * 24 / n_lists_call;

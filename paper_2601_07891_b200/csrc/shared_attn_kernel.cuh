@@ -79,8 +79,14 @@ __device__ __forceinline__ int share_ctas(int64_t tiles, int n_ctas)
     return static_cast<int>(want < n_ctas ? (want > 0 ? want : 1) : n_ctas);
 }
 __device__ __forceinline__ int64_t share_run(int64_t tiles, int ctas, int i) { return tiles * i / ctas; }
-// the CTA whose run tile t is in
-__device__ __forceinline__ int share_owner(int64_t tiles, int ctas, int64_t t) { return static_cast<int>(((t + 1) * ctas - 1) / tiles); }
+// the CTA whose run tile t is in: the last i with tiles * i / ctas <= t, from an estimate (a 64-bit division takes as long as a load)
+__device__ __forceinline__ int share_owner(int64_t tiles, int ctas, int64_t t)
+{
+    int i = static_cast<int>(static_cast<float>(t) * static_cast<float>(ctas) / static_cast<float>(tiles));
+    while (i > 0 && tiles * i >= (t + 1) * ctas) --i;
+    while (tiles * (i + 1) < (t + 1) * ctas) ++i;
+    return i;
+}
 
 __host__ __device__ constexpr int sh_stages(int d) { return d == 128 ? 5 : 9; }
 __host__ __device__ constexpr uint32_t sh_stage_bytes(int d) { return kShTile * d * 2u; }
@@ -285,43 +291,42 @@ __device__ __forceinline__ ShareRun share_my_run(const SharedAttnParams &p)
     __shared__ int unit_s;
     const int per_layer = p.v.n_subs * p.c.n_heads, n_units = p.n_layers_call * per_layer;
     const int4 *lists = p.v.lists + static_cast<int64_t>(p.layer0) * per_layer;
-    const bool grouped = *p.v.stamp_now == p.v.stamp;
-    ShareRun r{0, 0, lists[0].x, 0};
-    const int64_t tiles = grouped ? lists[n_units].x - r.base : 0;
+    const int32_t stamp = __ldg(p.v.stamp_now);
+    ShareRun r{0, 0, __ldg(&lists[0].x), 0};
+    const int64_t tiles = stamp == p.v.stamp ? __ldg(&lists[n_units].x) - r.base : 0;
     const int ctas = share_ctas(tiles, p.v.n_ctas);
     if (static_cast<int>(blockIdx.x) < ctas) {
         r.at = share_run(tiles, ctas, blockIdx.x);
         r.end = share_run(tiles, ctas, blockIdx.x + 1);
     }
     for (int u = threadIdx.x; u < n_units; u += kShThreads) {
-        const int64_t first = lists[u].x - r.base, last = lists[u + 1].x - r.base;
+        const int64_t first = __ldg(&lists[u].x) - r.base, last = __ldg(&lists[u + 1].x) - r.base;
         if (first <= r.at && r.at < last) unit_s = u;
     }
     __syncthreads();
     if (r.at < r.end) r.unit = unit_s;
     return r;
 }
-// False: the run is over.
+// False: the run is over.  Lists that no member shares any more are left out.
 __device__ __forceinline__ bool share_next(const SharedAttnParams &p, ShareRun &r, SharePiece &x)
 {
-    if (r.at >= r.end) return false;
     const int4 *lists = p.v.lists + static_cast<int64_t>(p.layer0) * p.v.n_subs * p.c.n_heads;
-    int4 mine = __ldg(lists + r.unit);
-    int32_t next = __ldg(&lists[r.unit + 1].x);
-    while (next - r.base <= r.at) {                             // lists without tiles
-        mine = __ldg(lists + ++r.unit);
-        next = __ldg(&lists[r.unit + 1].x);
+    while (r.at < r.end) {
+        const int4 mine = __ldg(lists + r.unit);
+        const int64_t first = mine.x - r.base, last = __ldg(&lists[r.unit + 1].x) - r.base;
+        x.unit = r.unit;
+        x.t0 = static_cast<int>(r.at - first);
+        x.t1 = static_cast<int>((last < r.end ? last : r.end) - first);
+        x.n_rows = mine.y;
+        x.leader = mine.z;
+        x.m0 = mine.w >> 9;
+        x.n_mem = mine.w & 511;
+        r.unit += 1;
+        if (last <= r.at) continue;                                 // no tiles
+        r.at = first + x.t1;
+        if (mine.y > 0) return true;
     }
-    const int64_t first = mine.x - r.base, last = next - r.base;
-    x.unit = r.unit;
-    x.t0 = static_cast<int>(r.at - first);
-    x.t1 = static_cast<int>((last < r.end ? last : r.end) - first);
-    x.n_rows = mine.y;
-    x.leader = mine.z;
-    x.m0 = mine.w >> 9;
-    x.n_mem = mine.w & 511;
-    r.at = first + x.t1;
-    return true;
+    return false;
 }
 
 // Registers of the calling warpgroup from here on.  The block is launched with 384 x 168; 256 x 216 + 128 x 72 is the same.
@@ -404,7 +409,6 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const uint64_t policy = l2_policy_evict_first();
         const uint32_t box_bytes = p.box_rows * 128u;
         while (ok && share_next(p, walk, x)) {
-            if (x.n_rows == 0) continue;
             const int n = x.t1 - x.t0;
             const int32_t *pages = c.page_table + static_cast<int64_t>(x.leader) * c.max_pages;
             // of this lane's box of tile t: its page and its first row there (-1: no such box); the page number is on its way while the tiles
@@ -448,7 +452,6 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             return ok;
         };
         while (ok && share_next(p, walk, x)) {
-            if (x.n_rows == 0) continue;
             const int n = x.t1 - x.t0;
             const bool two = x.n_mem * p.group > 128;
             const int steps = two ? 2 * n : n;
@@ -516,85 +519,87 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
         uint32_t n_s = 0, n_piece = 0;
-        bool told = false;                                        // the producers
-        while (share_next(p, walk, x)) {
+        // The piece's rows of Q, 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros.  Sent for while the piece before is
+        // brought to its end (there are no registers to load them to).
+        constexpr int kUnits = kD / 8;
+        auto queries = [&](const SharePiece &y, uint4 *q) {       // q == nullptr: only sends for them
+            const int n_rows_q = y.n_mem * p.group;
+            const bool two = n_rows_q > 128;
+            const int first = two ? w * 128 : 0, n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
+            const int h = y.unit % c.n_heads, l = y.unit / (c.n_heads * p.v.n_subs);
+            const int64_t heads = static_cast<int64_t>(c.n_heads) * p.group;
+            const uint16_t *base = p.q + (static_cast<int64_t>(l) * c.n_seqs * heads + h * p.group) * kD;
+            // all loads of a kind go out together: rows past the members' read the last one's
+            int32_t seq[kUnits], head[kUnits];
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const int qr = min(first + (at + k * n_thr) / kUnits, n_rows_q - 1), m = qr / p.group;
+                head[k] = qr - m * p.group;
+                seq[k] = __ldg(p.sub_seqs + y.m0 + m);
+            }
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const uint4 *at_q = reinterpret_cast<const uint4 *>(base + (seq[k] * heads + head[k]) * kD) + (at + k * n_thr) % kUnits;
+                if (q != nullptr) q[k] = __ldg(at_q);
+                else if (lane % 8 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(at_q));
+            }
+            if (q != nullptr)
+#pragma unroll
+                for (int k = 0; k < kUnits; ++k)
+                    if (first + (at + k * n_thr) / kUnits >= n_rows_q) q[k] = make_uint4(0u, 0u, 0u, 0u);
+        };
+        bool have = share_next(p, walk, x);
+        if (!have) named_barrier_arrive(4, 256 + 32 * kShProducers);
+        while (have) {
             const int n_rows_q = x.n_mem * p.group;
             const bool two = n_rows_q > 128;
             const int slot = static_cast<int>(blockIdx.x) + x.unit;
             const int64_t out_row = static_cast<int64_t>(slot) * p.v.rows_max;
             float2 *ml_out = const_cast<float2 *>(p.v.part_ml) + out_row;
-            if (!ok) {                                            // a wait ran out: the outputs that this piece is part of are zeros
-                for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
-                if (x.n_rows > 0) {                               // as many as of each piece that is worked on, whoever gave up when
-                    named_barrier_sync(1, 256);
-                    named_barrier_sync(1, 256);
-                }
-                continue;
-            }
-            if (x.n_rows == 0) continue;
-            // Q: 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros.  What a group of warps has left there of the
-            // piece before has been copied out.
+            uint4 q[kUnits];
+            queries(x, q);
+            if (n_piece == 0) named_barrier_arrive(4, 256 + 32 * kShProducers);
+            // What a group of warps has left in its tile of Q of the piece before has been copied out.
             bulk_wait_read();
             named_barrier_sync(1, 256);
             {
-                constexpr int kUnits = kD / 8, kBatch = 8;
-                const int first = two ? w * 128 : 0, n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
-                const int h = x.unit % c.n_heads, l = x.unit / (c.n_heads * p.v.n_subs);
-                const int64_t heads = static_cast<int64_t>(c.n_heads) * p.group;
-                const uint16_t *q = p.q + (static_cast<int64_t>(l) * c.n_seqs * heads + h * p.group) * kD;
+                const int n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
                 uint8_t *tile = smem + (kStages + (two ? w : 0)) * kStageBytes;
-                for (int i0 = at; i0 < 128 * kUnits; i0 += n_thr * kBatch) {
-                    uint4 v[kBatch];
 #pragma unroll
-                    for (int k = 0; k < kBatch; ++k) {
-                        const int i = i0 + k * n_thr, qr = first + i / kUnits;
-                        v[k] = make_uint4(0u, 0u, 0u, 0u);
-                        if (i < 128 * kUnits && qr < n_rows_q) {
-                            const int m = qr / p.group;
-                            v[k] = __ldg(reinterpret_cast<const uint4 *>(q + (__ldg(p.sub_seqs + x.m0 + m) * heads + (qr - m * p.group)) * kD) + i % kUnits);
-                        }
-                    }
-                    if (!told) named_barrier_arrive(4, 256 + 32 * kShProducers);
-                    told = true;
-#pragma unroll
-                    for (int k = 0; k < kBatch; ++k) {
-                        const int i = i0 + k * n_thr, r = i / kUnits, u = i % kUnits;
-                        if (i < 128 * kUnits)
-                            *reinterpret_cast<uint4 *>(tile + (u >> 3) * kHalfBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4)) = v[k];
-                    }
+                for (int k = 0; k < kUnits; ++k) {
+                    const int i = at + k * n_thr, r = i / kUnits, u = i % kUnits;
+                    if (k < kUnits / 2 || two)
+                        *reinterpret_cast<uint4 *>(tile + (u >> 3) * kHalfBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4)) = q[k];
                 }
                 fence_proxy_async_smem();
                 mbar_arrive(q_full);
             }
             const int n = x.t1 - x.t0, mine = two ? n : (n + 1 - w) / 2;
             float m_ref = -INFINITY, l_run = 0.0f;
-            for (int i = 0; i < mine; ++i) {
+            for (int i = 0; ok && i < mine; ++i) {
                 const int t = two ? i : 2 * i + w;
                 if (!__all_sync(0xffffffffu, mbar_wait(s_full + 8 * w, n_s & 1, &abort_s))) { ok = false; break; }
                 n_s += 1;
                 tc_fence_after_sync();
                 const int rows = x.n_rows - (x.t0 + t) * kShTile;
-                uint32_t s[128];
+                // the row in pieces of 32 columns, from tensor memory twice: rolled, the code of a step is there after a few misses of the instruction cache
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int j = 0; j < 4; j += 2) {
+                    uint32_t s[64];
+                    tmem_ld_x32(ts + 32 * j, s);
+                    tmem_ld_x32(ts + 32 * j + 32, s + 32);
+                    tmem_wait_ld();
+                    reg_fence32(s);
+                    reg_fence32(s + 32);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tmem_ld_x32(ts + 32 * j, s + 32 * j);
-                tmem_wait_ld();
+                    for (int g = 0; g < 4; ++g) {
+                        float m16 = fmaxf(__uint_as_float(s[16 * g]), __uint_as_float(s[16 * g + 1]));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) reg_fence32(s + 32 * j);
-                if (rows < kShTile) {                            // past the list's end (rows is a multiple of 16)
-#pragma unroll
-                    for (int j = 16; j < kShTile; ++j)
-                        if (j / 16 * 16 >= rows) s[j] = 0xff800000u;
+                        for (int k = 2; k < 16; k += 2) m16 = fmaxf(m16, fmaxf(__uint_as_float(s[16 * g + k]), __uint_as_float(s[16 * g + k + 1])));
+                        if (32 * j + 16 * g < rows) mx = fmaxf(mx, m16);
+                    }
                 }
-                float mx4[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mx4[j] = __uint_as_float(s[j]);
-#pragma unroll
-                for (int j = 4; j < kShTile; j += 8) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        mx4[k] = fmaxf(mx4[k], j + 4 + k < kShTile ? fmaxf(__uint_as_float(s[j + k]), __uint_as_float(s[j + 4 + k])) : __uint_as_float(s[j + k]));
-                }
-                float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx *= p.scale_log2e;
                 if (i == 0) {
                     m_ref = mx;
@@ -619,27 +624,36 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const float m_use = m_ref == -INFINITY ? 0.0f : m_ref;
                 const uint64_t scale2 = f2_pack(p.scale_log2e, p.scale_log2e), minus_m = f2_pack(-m_use, -m_use);
                 float sum = 0.0f;
+#pragma unroll 1
+                for (int j = 0; j < 4; j += 2) {
+                    uint32_t s[64];
+                    tmem_ld_x32(ts + 32 * j, s);
+                    tmem_ld_x32(ts + 32 * j + 32, s + 32);
+                    tmem_wait_ld();
+                    reg_fence32(s);
+                    reg_fence32(s + 32);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {                    // 16 columns at a time
-                    uint32_t pk[8];
-                    uint64_t sum2 = 0, sum2b = 0;
+                    for (int g = 0; g < 4; ++g) {                // 16 columns at a time
+                        uint32_t pk[8];
+                        uint64_t sum2 = 0, sum2b = 0;
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) {
-                        const uint32_t *v = s + 16 * j + k;
-                        float a, b, d, e;
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, minus_m), a, b);
-                        f2_unpack(f2_fma(f2_pack(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, minus_m), d, e);
-                        a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
-                        sum2 = k == 0 ? f2_pack(a, b) : f2_add(sum2, f2_pack(a, b));
-                        sum2b = k == 0 ? f2_pack(d, e) : f2_add(sum2b, f2_pack(d, e));
-                        pk[k / 2] = pack_bf16x2(a, b);           // P: 8 bits, relative to the row's maximum; the sum takes all 24
-                        pk[k / 2 + 1] = pack_bf16x2(d, e);
+                        for (int k = 0; k < 16; k += 4) {
+                            const uint32_t *v = s + 16 * g + k;
+                            float a, b, d, e;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, minus_m), a, b);
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, minus_m), d, e);
+                            a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
+                            sum2 = k == 0 ? f2_pack(a, b) : f2_add(sum2, f2_pack(a, b));
+                            sum2b = k == 0 ? f2_pack(d, e) : f2_add(sum2b, f2_pack(d, e));
+                            pk[k / 2] = pack_bf16x2(a, b);       // P: 8 bits, relative to the row's maximum; the sum takes all 24
+                            pk[k / 2 + 1] = pack_bf16x2(d, e);
+                        }
+                        float a, b;
+                        f2_unpack(f2_add(sum2, sum2b), a, b);
+                        if (32 * j + 16 * g < rows) sum += a + b;    // past the end: no numbers at a scale of zero, and not read by the product
+                        tmem_st_x8(ts + 16 * j + 8 * g, pk);
                     }
-                    float a, b;
-                    f2_unpack(f2_add(sum2, sum2b), a, b);
-                    if (16 * j < rows) sum += a + b;             // past the end: no numbers at a scale of zero, and not read by the product
-                    tmem_st_x8(ts + 8 * j, pk);
-                    if (j == 3) {                                // the product takes the first half while the second is worked out
+                    if (j == 0) {                                // the product takes the first half while the second is worked out
                         tmem_wait_st();
                         tc_fence_before_sync();
                         mbar_arrive(p_full + 16 * w);
@@ -650,6 +664,9 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 tc_fence_before_sync();
                 mbar_arrive(p_full + 16 * w + 8);
             }
+            SharePiece after;
+            have = share_next(p, walk, after);
+            if (have) queries(after, nullptr);
             if (ok && !__all_sync(0xffffffffu, mbar_wait(done, n_piece & 1, &abort_s))) ok = false;
             tc_fence_after_sync();
             // the groups tell one another their (m, l) where S was
@@ -662,7 +679,8 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             tc_fence_after_sync();
             if (failed_s) ok = false;
             n_piece += 1;
-            if (!ok) {
+            x = after;
+            if (!ok) {                                            // a wait ran out: the outputs that this piece is part of are zeros
                 for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);
                 continue;
             }
@@ -733,7 +751,6 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             tc_fence_before_sync();
             mbar_arrive(o_free);
         }
-        if (!told) named_barrier_arrive(4, 256 + 32 * kShProducers);
         bulk_wait();
         if (!ok && threadIdx.x % 128 == 0) atomicCAS(p.status, 0, 5 /* KVZAP_ERR_TIMEOUT */);
     }
