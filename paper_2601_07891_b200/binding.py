@@ -150,8 +150,15 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# The current stream's handle without the objects around it (a tenth of the time), where this torch has the call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+            return ctypes.c_void_p(_raw_stream(_raw_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -441,15 +448,18 @@ def kvzap_set_rotary(handle, head_dim, rotary_dim, base=10000.0, interleaved=Fal
 def rotary_rows(x, out, rotate):
     """One tensor of kvzap_rotary: x [T, heads, D] bf16 -> out [T, heads, D] bf16 or [T, heads, D + 16] uint8 (8-bit rows); views with any
     strides whose last dimension is contiguous."""
-    rows8 = out.dtype == torch.uint8
-    want = x.shape[:2] + ((x.shape[2] + 16,) if rows8 else x.shape[2:])
-    if x.dim() != 3 or x.dtype != torch.bfloat16 or (not rows8 and out.dtype != torch.bfloat16) or tuple(out.shape) != tuple(want):
+    shape, out_shape, out_type = x.shape, out.shape, out.dtype
+    rows8 = out_type is torch.uint8
+    if len(shape) != 3 or len(out_shape) != 3 or x.dtype is not torch.bfloat16 or not (rows8 or out_type is torch.bfloat16) or \
+            out_shape[0] != shape[0] or out_shape[1] != shape[1] or out_shape[2] != shape[2] + (16 if rows8 else 0):
         raise ValueError("rows must be bf16 [T, heads, D] -> bf16 of that shape or uint8 [T, heads, D + 16], got %s -> %s" % (
-            tuple(x.shape), tuple(out.shape)))
-    if not x.is_cuda or out.device != x.device or (x.numel() and (x.stride(2) != 1 or out.stride(2) != 1)):
+            tuple(shape), tuple(out_shape)))
+    some = shape[0] > 0 and shape[1] > 0 and shape[2] > 0
+    at, out_at = x.stride(), out.stride()
+    if not x.is_cuda or out.get_device() != x.get_device() or (some and (at[2] != 1 or out_at[2] != 1)):
         raise ValueError("rows must lie on one CUDA device, their elements side by side")
-    return KvzapRows(x.data_ptr() if x.numel() else None, out.data_ptr() if x.numel() else None, x.stride(0), x.stride(1),
-                     out.stride(0), out.stride(1), x.shape[1], (ROWS_ROTATE if rotate else 0) | (ROWS_8BIT if rows8 else 0))
+    return KvzapRows(x.data_ptr() if some else None, out.data_ptr() if some else None, at[0], at[1], out_at[0], out_at[1], shape[1],
+                     (ROWS_ROTATE if rotate else 0) | (ROWS_8BIT if rows8 else 0))
 
 
 def kvzap_rotary(handle, positions, rows, inverse=False, stream=None):
@@ -675,6 +685,7 @@ class Kvzap:
         consecutive calls.  Off, a call's first kernel waits for the work ahead of it in the stream."""
         self.d_model, self.hidden, self.n_kv_heads, self.head_dim = d_model, hidden, n_kv_heads, head_dim
         self.n_layers, self.max_tokens, self.max_seqs = n_layers, max_tokens, max_seqs
+        self._rotary_head_dim = None
         self.device = torch.device("cuda", device)
         self.handle = kvzap_create(d_model, hidden, n_kv_heads, head_dim, n_layers, max_tokens, max_seqs, device,
                                    FLAG_TRUSTED_PRODUCERS if trusted_producers else 0)
@@ -784,12 +795,14 @@ class Kvzap:
         buffer gives the layout of the pruning calls), or uint8 [T, heads, D + 16] given for 8-bit rows.  Returns those of the given inputs."""
         if positions.dim() != 1 or positions.dtype != torch.int32:
             raise ValueError("positions must be int32 [T]")
+        n_tokens = positions.shape[0]
         rows, outs = [], []
         for x, out, rotate in ((Q, Q_out, True), (K, K_out, True), (V, V_out, False)):
             if x is None:
                 continue
-            if x.dim() != 3 or x.shape[0] != positions.shape[0] or x.shape[2] != getattr(self, "_rotary_head_dim", x.shape[2]):
-                raise ValueError("rows must be [%d, heads, %s], got %s" % (positions.shape[0], getattr(self, "_rotary_head_dim", "D"), tuple(x.shape)))
+            shape = x.shape
+            if len(shape) != 3 or shape[0] != n_tokens or shape[2] != (self._rotary_head_dim or shape[2]):
+                raise ValueError("rows must be [%d, heads, %s], got %s" % (n_tokens, self._rotary_head_dim or "D", tuple(shape)))
             if out is None:
                 out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
             rows.append(rotary_rows(x, out, rotate))

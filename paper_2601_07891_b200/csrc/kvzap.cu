@@ -3293,7 +3293,8 @@ static kvzap_status launch_pack(kvzap_cache *cache, const PackArgs &a, const Slo
 {
     kvzap_ctx *ctx = cache->ctx;
     const size_t smem = sizeof(int64_t) * (static_cast<size_t>(a.n_lists) + 1);
-    KVZAP_CUDA(ctx, cudaFuncSetAttribute(pack_kernel<kOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(int64_t) * (kPackLists + 1))));
+    if (smem > 48 * 1024)
+        KVZAP_CUDA(ctx, cudaFuncSetAttribute(pack_kernel<kOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(int64_t) * (kPackLists + 1))));
     const int per_sm = smem <= 24 * 1024 ? 8 : smem <= 96 * 1024 ? 2 : 1;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attrs[2];

@@ -519,34 +519,31 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
         uint32_t n_s = 0, n_piece = 0;
-        // The piece's rows of Q, 16 bytes a thread, the lanes of a warp along the rows; rows past the members' are zeros.  Sent for while the piece before is
-        // brought to its end (there are no registers to load them to).
-        constexpr int kUnits = kD / 8;
-        auto queries = [&](const SharePiece &y, uint4 *q) {       // q == nullptr: only sends for them
+        // The piece's rows of Q: of one tile 16 a warp, of two 32; a lane finds the place of one of them (in units of 16 bytes), then 32 lanes load whole
+        // rows.  Rows past the members' read the last one's, and are zeros.  Sent for while the piece before is brought to its end (there are no
+        // registers to load them to).  Short code: in a launch's first microseconds instructions are waited for like data.
+        constexpr int kUnits = kD / 8, kRowsAt = 32 / kUnits;        // rows loaded at a time
+        auto queries = [&](const SharePiece &y, uint4 *q) {          // q == nullptr: only sends for them
             const int n_rows_q = y.n_mem * p.group;
             const bool two = n_rows_q > 128;
-            const int first = two ? w * 128 : 0, n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
+            const int row0 = (two ? 32 : 16) * warp;
+            const int qr = min(row0 + (two ? lane : lane & 15), n_rows_q - 1), m = qr / p.group;
             const int h = y.unit % c.n_heads, l = y.unit / (c.n_heads * p.v.n_subs);
-            const int64_t heads = static_cast<int64_t>(c.n_heads) * p.group;
-            const uint16_t *base = p.q + (static_cast<int64_t>(l) * c.n_seqs * heads + h * p.group) * kD;
-            // all loads of a kind go out together: rows past the members' read the last one's
-            int32_t seq[kUnits], head[kUnits];
+            const int heads = c.n_heads * p.group;
+            const int64_t place = (static_cast<int64_t>(l) * c.n_seqs + __ldg(p.sub_seqs + y.m0 + m)) * heads + h * p.group + (qr - m * p.group);
+            const uint4 *at_q = reinterpret_cast<const uint4 *>(p.q) + place * kUnits;
+            if (q == nullptr) {
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k) {
-                const int qr = min(first + (at + k * n_thr) / kUnits, n_rows_q - 1), m = qr / p.group;
-                head[k] = qr - m * p.group;
-                seq[k] = __ldg(p.sub_seqs + y.m0 + m);
+                for (int k = 0; k < kD * 2; k += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const uint8_t *>(at_q) + k));
+                return;
             }
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const uint4 *at_q = reinterpret_cast<const uint4 *>(base + (seq[k] * heads + head[k]) * kD) + (at + k * n_thr) % kUnits;
-                if (q != nullptr) q[k] = __ldg(at_q);
-                else if (lane % 8 == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(at_q));
+                const int r = kRowsAt * k + lane / kUnits;
+                const uint4 *from = reinterpret_cast<const uint4 *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(at_q), r & 31));
+                q[k] = __ldg(from + lane % kUnits);                  // of one tile the second half is not used
+                if (row0 + r >= n_rows_q) q[k] = make_uint4(0u, 0u, 0u, 0u);
             }
-            if (q != nullptr)
-#pragma unroll
-                for (int k = 0; k < kUnits; ++k)
-                    if (first + (at + k * n_thr) / kUnits >= n_rows_q) q[k] = make_uint4(0u, 0u, 0u, 0u);
         };
         bool have = share_next(p, walk, x);
         if (!have) named_barrier_arrive(4, 256 + 32 * kShProducers);
@@ -563,11 +560,10 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             bulk_wait_read();
             named_barrier_sync(1, 256);
             {
-                const int n_thr = two ? 128 : 256, at = two ? threadIdx.x - w * 128 : threadIdx.x;
                 uint8_t *tile = smem + (kStages + (two ? w : 0)) * kStageBytes;
 #pragma unroll
                 for (int k = 0; k < kUnits; ++k) {
-                    const int i = at + k * n_thr, r = i / kUnits, u = i % kUnits;
+                    const int r = (two ? 32 * (warp & 3) : 16 * warp) + kRowsAt * k + lane / kUnits, u = lane % kUnits;
                     if (k < kUnits / 2 || two)
                         *reinterpret_cast<uint4 *>(tile + (u >> 3) * kHalfBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4)) = q[k];
                 }
