@@ -350,6 +350,17 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         return stamp == p.share.stamp ? rows : 0;
     };
     int32_t n_shared = 0;                   // kShared: of this list
+    // ... its group, its place there, tiles ahead of the call and in it: looked up beside the lengths
+    int sh_sub = 0, sh_row = 0;
+    int32_t sh_base = 0, sh_end = 0;
+    auto look_up_group = [&](int i) {
+        const int b = (i / H) % B;
+        const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
+        sh_sub = __ldcg(p.share.seq_sub + b);
+        sh_row = __ldcg(p.share.seq_pos + b) * p.group;
+        sh_base = __ldcg(&lists[0].x);
+        sh_end = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x);
+    };
     if (kShared && n_parts > 0) {
         auto tiles_of = [&](int i) {
             const int64_t li = cache_list(i);
@@ -361,6 +372,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             n_total = __ldcg(c.n_tokens + cache_list(i));
             n_prefix = __ldcg(c.prefix_len + cache_list(i));
             n_shared = shared_rows(i);
+            look_up_group(i);
         };
         if (mine.list < p.extra0) look_up(mine.list);
         if (mine.list >= p.extra0 || n_prefix - n_shared + min(n_total, c.window) > kAttnLongTiles * kAttnTileRows - 2 * kAttnTileRows) {
@@ -435,6 +447,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         n_before = n_prefix = counts[list].x;
         n_total = counts[list].y;
         n_shared = shared_rows(list);
+        if constexpr (kShared) look_up_group(list);
         if (kBeside && !beside) n_prefix = __ldcg(c.prefix_len + cache_list(list));
         fence_proxy_async_smem();                                  // the copies below write where these were read
         __syncthreads();
@@ -658,20 +671,23 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         asm volatile("" ::"r"(seen) : "memory");
         if (lane == 0 && atomicAdd(&queries_s, 1) == kAttnWarps - 1) griddep_launch_dependents();
     };
-    // kShared: the slots of the list's shared rows (looked up while the first rows are on their way)
-    int sh_slot = 0, sh_row = 0, sh_n = 0;
+    // kShared: the list's slots; its tiles are on their way beside the first page numbers
+    int sh_slot = 0, sh_n = 0;
+    int32_t sh_first = 0, sh_last = 0;
+    if constexpr (kShared) {
+        const int64_t unit = (static_cast<int64_t>(list / (H * B)) * p.share.n_subs + sh_sub) * H + list % H;
+        const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H + unit;
+        sh_first = __ldcg(&lists[0].x);
+        sh_last = __ldcg(&lists[1].x);
+        sh_slot = static_cast<int>(unit);
+    }
     auto find_shared = [&]() {
-        if (n_shared > 0) {
-            const int h = list % H, b = (list / H) % B, l = list / (H * B);
-            const int unit = (l * p.share.n_subs + __ldcg(p.share.seq_sub + b)) * H + h;
-            const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
-            const int64_t base = __ldcg(&lists[0].x), tiles = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x) - base;
-            const int ctas = share_ctas(tiles, p.share.n_ctas);
-            const int c0 = share_owner(tiles, ctas, __ldcg(&lists[unit].x) - base), c1 = share_owner(tiles, ctas, __ldcg(&lists[unit + 1].x) - base - 1);
-            sh_slot = c0 + unit;
-            sh_row = __ldcg(p.share.seq_pos + b) * p.group;
-            sh_n = c1 - c0 + 1;
-        }
+        if (n_shared == 0) return;
+        const int64_t tiles = sh_end - sh_base;
+        const int ctas = share_ctas(tiles, p.share.n_ctas);
+        const int c0 = share_owner(tiles, ctas, sh_first - sh_base);
+        sh_slot += c0;
+        sh_n = share_owner(tiles, ctas, sh_last - sh_base - 1) - c0 + 1;
     };
     float o[kNTiles][4];
     float m_run = 0.0f, l_run = 0.0f;
