@@ -9,11 +9,14 @@
 // signed multiple of 2^-31 half turns, go to sincospif: an angle is off by 2^-32 turns + the rounding to fp32, at any position,
 // without a 64-bit sine and without a table of positions.
 //
-// Bound by reading each row once and writing it once.  A thread has 8 pairs (two 16-byte pieces of a head) of one token, works
-// their sines out once and goes over the token's heads, of all tensors of the call, with them.
+// Bound by reading each row once and writing it once: 32768 tokens, 32 + 8 heads of 128, 671 MB, 108 us (6.2 TB/s).  A thread has 8 pairs (two
+// 16-byte pieces of a head) of one token, works their sines out once and goes over the token's heads, of all tensors of the call, with
+// them, the next row on its way while one is worked out.  Us, that prompt / 7777 tokens with half of each head rotated / 16411 tokens with keys and
+// values to 8-bit rows: 108 / 31 / 69; without the row ahead 120 / 33 / 84 (the last also with 16 divisions a thread, now one reciprocal); at 78
+// registers, three quarters of the threads, 115 / 35 / 73; half a warp for a token 117 / 32 / 72, two warps 131 / 35 / 80.
 //
 // 8-bit rows (D E4M3 codes, then the fp32 scale and 12 zero bytes): scale = the row's largest magnitude / 448 (1 for a row of
-// zeros), codes rounded to nearest from the fp32 result, which is rounded nowhere before.
+// zeros), codes rounded to nearest from the fp32 result (times the scale's reciprocal), which is rounded nowhere before.
 #pragma once
 
 #include "ptx.cuh"
@@ -21,7 +24,7 @@
 namespace kvzap {
 
 constexpr int kRotTensors = 3;
-constexpr int kRotThreads = 256;
+constexpr int kRotThreads = 128;
 constexpr uint32_t kRotRotate = 1u, kRotRows8 = 2u;           // as KVZAP_ROWS_*
 
 struct RotaryTensor {
@@ -61,7 +64,7 @@ __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi)
 
 // head_dim and rotary_dim multiples of 16, everything 16-byte aligned.
 template <int kPairs, bool kInterleaved>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 8)
 rotary_kernel(const __grid_constant__ RotaryParams<kPairs> p)
 {
     griddep_wait();                   // and lets nothing start before it is done: its outputs are the next call's inputs
@@ -81,26 +84,34 @@ rotary_kernel(const __grid_constant__ RotaryParams<kPairs> p)
     float c[8], s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
+    // Every thread of a warp goes along: rows of 8 bits are worked out by several.  The next head's row is on its way while one is worked out.
+    const int n_rounds = (p.n_heads + p.rows - 1) / p.rows;
+    int next_h = row, next_t = 0;                              // head of the call, then of tensor next_t
+    auto step = [&](uint4 &a, uint4 &b) {
+        while (next_t < p.n_tensors && next_h >= p.t[next_t].n_heads) { next_h -= p.t[next_t].n_heads; ++next_t; }
+        a = b = make_uint4(0u, 0u, 0u, 0u);
+        if (there && next_t < p.n_tensors) {
+            const RotaryTensor &t = p.t[next_t];
+            const uint8_t *src = t.in + token * t.in_token + next_h * t.in_head;
+            a = *reinterpret_cast<const uint4 *>(src + 2 * e0);
+            b = *reinterpret_cast<const uint4 *>(src + 2 * e1);
+        }
+    };
+    uint4 next_a, next_b;
+    step(next_a, next_b);
     if (turn) {
         const int32_t position = p.positions[token];
 #pragma unroll
         for (int i = 0; i < 8; ++i) rotary_turn(p.step[8 * j + i], position, p.magnitude, p.sign, c[i], s[i]);
     }
-    int h = row;                                               // head of the call, then of tensor t
-    const int n_rounds = (p.n_heads + p.rows - 1) / p.rows;
-    int ti = 0;
-#pragma unroll 1
-    for (int round = 0; round < n_rounds; ++round, h += p.rows) {
-        // every thread of a warp goes along: rows of 8 bits are worked out by several
-        while (ti < p.n_tensors && h >= p.t[ti].n_heads) { h -= p.t[ti].n_heads; ++ti; }
+#pragma unroll 2
+    for (int round = 0; round < n_rounds; ++round) {
+        const int h = next_h, ti = next_t;
         const bool work = there && ti < p.n_tensors;
         const RotaryTensor &t = p.t[ti < p.n_tensors ? ti : 0];
-        uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-        if (work) {
-            const uint8_t *src = t.in + token * t.in_token + h * t.in_head;
-            a = *reinterpret_cast<const uint4 *>(src + 2 * e0);
-            b = *reinterpret_cast<const uint4 *>(src + 2 * e1);
-        }
+        const uint4 a = next_a, b = next_b;
+        next_h += p.rows;
+        step(next_a, next_b);
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         float x[16];
 #pragma unroll
@@ -132,11 +143,19 @@ rotary_kernel(const __grid_constant__ RotaryParams<kPairs> p)
             for (int o = 1; o < p.lanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));      // 4 or 8 lanes a row
             if (work && (t.flags & kRotRows8)) {
                 const float scale = top > 0.0f ? __fdiv_rn(top, 448.0f) : 1.0f;
+                // times the reciprocal, 2^-23 off the quotient; it is no number for the smallest scales
                 uint32_t y[4];
+                if (scale >= 1.0e-37f) {
+                    const float inv = __frcp_rn(scale);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] *= inv;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], scale);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    y[i] = pack_e4m3x2(__fdiv_rn(x[4 * i], scale), __fdiv_rn(x[4 * i + 1], scale)) |
-                           pack_e4m3x2(__fdiv_rn(x[4 * i + 2], scale), __fdiv_rn(x[4 * i + 3], scale)) << 16;
+                    y[i] = pack_e4m3x2(x[4 * i], x[4 * i + 1]) | pack_e4m3x2(x[4 * i + 2], x[4 * i + 3]) << 16;
                 *reinterpret_cast<uint2 *>(dst + e0) = make_uint2(y[0], y[1]);
                 *reinterpret_cast<uint2 *>(dst + e1) = make_uint2(y[2], y[3]);
                 if (j == 0) *reinterpret_cast<uint4 *>(dst + p.head_dim) = make_uint4(__float_as_uint(scale), 0u, 0u, 0u);
