@@ -182,24 +182,29 @@ __device__ __forceinline__ int attn_unit(const int32_t *lengths, int n, int n_un
     return __shfl_sync(0xffffffffu, parts, src);
 }
 
-// kShared, more lists than CTAs find room: how long a list's own rows are the host does not know, and what members have added since they were
-// forked is mostly little beside what the lists could hold.  Every list has a CTA; one of more than kAttnLongTiles tiles has as many parts as
-// make that many tiles each, for which a wave of further CTAs stands by at the end of the launch.  If those do not suffice the length of a part is
-// doubled until they do.  Only CTAs of long lists and the further ones look at all lists (some 2 us); the others know by themselves that
-// they are alone.
-constexpr int kAttnLongTiles = 64;
+// kShared: a list is worked on by a single warp, several lists side by side in a CTA, with nothing shared between warps at all: what members have added
+// since they were forked is mostly little, and a CTA for each such list spent two thirds of its time on what comes before and behind the
+// rows.  A list of more than kAttnWarpTiles tiles has as many parts as make that many tiles each, for which a wave of further CTAs stands by at
+// the end of the launch (the host does not know the lengths).  If those do not suffice the length of a part is doubled until they do.  Only CTAs with a
+// long list and the further ones look at all lists (some 2 us); the others know by themselves that they are alone.
+constexpr int kAttnWarpTiles = 24;
 constexpr int kAttnLongLevels = 24;
-struct AttnLong { int list, part, n_parts, unit0; };       // n_parts 0: nothing to do
-// Whole CTA; tiles_of(i): tiles of list i.  unit < n: the CTA of list `unit`, else a further one.  `tiles` in shared memory, for n lists, or nullptr.
+struct AttnUnit { int list, part, n_parts, unit0; };       // n_parts 0: nothing to do
+// Whole CTA: the units of its warps.  further = false: lists base + warp; else the parts base + warp of those that lists have beyond their first, n_more at most.
+// tiles_of(i): tiles of list i, n lists; `tiles`: room for them in shared memory, or nullptr.
 template <typename F>
-__device__ __forceinline__ AttnLong attn_long(int n, int n_more, int unit, F tiles_of, int32_t *tiles)
+__device__ __forceinline__ AttnUnit attn_warp_units(int n, int n_more, bool further, int base, F tiles_of, int32_t *tiles)
 {
-    __shared__ int more_s[kAttnLongLevels], sum_s[2][kAttnWarps], found_s[4];
+    __shared__ int more_s[kAttnLongLevels], sum_s[2][kAttnWarps];
+    __shared__ AttnUnit found_s[kAttnWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < kAttnLongLevels; i += kAttnThreads) more_s[i] = 0;
-    if (threadIdx.x == 0) found_s[2] = 0;
+    if (threadIdx.x < kAttnWarps) found_s[threadIdx.x] = {0, 0, 0, 0};
     __syncthreads();
-    auto parts_of = [&](int t, int level) { return max(1, static_cast<int>((t + (static_cast<int64_t>(kAttnLongTiles) << level) - 1) / (static_cast<int64_t>(kAttnLongTiles) << level))); };
+    auto parts_of = [&](int t, int level) {
+        const int64_t most = static_cast<int64_t>(kAttnWarpTiles) << level;
+        return t <= most ? 1 : static_cast<int>((t + most - 1) >> level) / kAttnWarpTiles;      // rounded up: most is kAttnWarpTiles 2^level
+    };
     auto get = [&](int i) { return tiles != nullptr ? tiles[i] : tiles_of(i); };
     constexpr int kBatch = 8;                                   // lists a thread looks up at a time
     for (int i0 = threadIdx.x; tiles != nullptr && i0 < n; i0 += kAttnThreads * kBatch) {
@@ -233,23 +238,19 @@ __device__ __forceinline__ AttnLong attn_long(int n, int n_more, int unit, F til
     __syncthreads();
     for (int w = 0; w < warp; ++w) { more_to += sum_s[0][w]; units_to += sum_s[1][w]; }
     int at = more_to - more, unit0 = units_to - units;
-    const int mine = unit - n;                                  // of the further parts
-    const bool has = unit < n ? unit % kAttnThreads == static_cast<int>(threadIdx.x) : at <= mine && mine < more_to;
-    if (has) {
+    if (!further || (at < base + kAttnWarps && base < more_to)) {
         for (int i = threadIdx.x; i < n; i += kAttnThreads) {
             const int parts = parts_of(get(i), level);
-            if (unit < n ? i == unit : parts > 1 && mine < at + parts - 1) {
-                found_s[0] = i;
-                found_s[1] = unit < n ? 0 : mine - at + 1;
-                found_s[2] = parts;
-                found_s[3] = unit0;
-                break;
+            if (!further) {
+                if (i >= base && i < base + kAttnWarps) found_s[i - base] = {i, 0, parts, unit0};
+            } else {
+                for (int e = max(at, base); e < min(at + parts - 1, base + kAttnWarps); ++e) found_s[e - base] = {i, e - at + 1, parts, unit0};
             }
             if (parts > 1) { at += parts - 1; unit0 += parts; }
         }
     }
     __syncthreads();
-    return {found_s[0], found_s[1], found_s[2], found_s[3]};
+    return found_s[warp];
 }
 
 constexpr int kAttnTrailerBytes = 16;            // 8-bit rows: fp32 scale + 12 unused bytes behind the codes
@@ -296,6 +297,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
                    const AttnParams p)
 {
     constexpr int kHalves = kD / 64;
+    constexpr int kStep = kShared ? 1 : kAttnWarps;                 // tiles from one of a warp's to its next
     constexpr int kAttnStages = attn_stages(kFp8);
     constexpr uint32_t kStageBytes = attn_stage_bytes(kD, kFp8);
     constexpr int kRowBytes8 = kD + kAttnTrailerBytes;              // 8-bit rows
@@ -361,28 +363,37 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         sh_base = __ldcg(&lists[0].x);
         sh_end = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x);
     };
-    if (kShared && n_parts > 0) {
+    if constexpr (kShared) {
         auto tiles_of = [&](int i) {
             const int64_t li = cache_list(i);
             const int32_t rows = __ldcg(c.prefix_len + li), tokens = __ldcg(c.n_tokens + li);
             return (rows - shared_rows(i) + kAttnTileRows - 1) / kAttnTileRows + (min(tokens, c.window) + kAttnTileRows - 1) / kAttnTileRows;
         };
-        AttnLong mine{static_cast<int>(blockIdx.x), 0, 1, 0};
         auto look_up = [&](int i) {
             n_total = __ldcg(c.n_tokens + cache_list(i));
             n_prefix = __ldcg(c.prefix_len + cache_list(i));
             n_shared = shared_rows(i);
             look_up_group(i);
         };
-        if (mine.list < p.extra0) look_up(mine.list);
-        if (mine.list >= p.extra0 || n_prefix - n_shared + min(n_total, c.window) > kAttnLongTiles * kAttnTileRows - 2 * kAttnTileRows) {
-            const bool fits = p.extra0 * 4 <= static_cast<int>(kAttnWarps * kAttnStages * kStageBytes);      // the stages are not in use yet
-            mine = attn_long(p.extra0, static_cast<int>(gridDim.x) - p.extra0, blockIdx.x, tiles_of, fits ? reinterpret_cast<int32_t *>(smem) : nullptr);
-            if (mine.n_parts == 0) return;                         // the whole CTA
+        const int n_lists = p.extra0, n_first = (n_lists + kAttnWarps - 1) / kAttnWarps;      // CTAs
+        const bool further = static_cast<int>(blockIdx.x) >= n_first;
+        AttnUnit mine{static_cast<int>(blockIdx.x) * kAttnWarps + warp, 0, 1, 0};
+        bool is_long = further;
+        if (!further && mine.list < n_lists) {
+            look_up(mine.list);
+            is_long = (n_prefix - n_shared + kAttnTileRows - 1) / kAttnTileRows + (min(n_total, c.window) + kAttnTileRows - 1) / kAttnTileRows > kAttnWarpTiles;
+        } else if (!further) {
+            mine.n_parts = 0;
+        }
+        if (__syncthreads_or(is_long)) {
+            const bool fits = n_lists * 4 <= static_cast<int>(kAttnWarps * kAttnStages * kStageBytes);      // the stages are not in use yet
+            mine = attn_warp_units(n_lists, (static_cast<int>(gridDim.x) - n_first) * kAttnWarps, further,
+                                   (static_cast<int>(blockIdx.x) - (further ? n_first : 0)) * kAttnWarps, tiles_of, fits ? reinterpret_cast<int32_t *>(smem) : nullptr);
             fence_proxy_async_smem();                              // the copies below write where the lengths were
             __syncthreads();
-            look_up(mine.list);
+            if (further && mine.n_parts > 0) look_up(mine.list);
         }
+        if (mine.n_parts == 0) return;                             // the whole warp; from here on no warp waits for another
         list = mine.list;
         part = mine.part;
         n_parts = mine.n_parts;
@@ -420,7 +431,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             int2 n = make_int2(__ldcg(before + cache_list(i)), beside ? 0 : __ldcg(c.n_tokens + cache_list(i)));
             if (kBeside) n.x = min(n.x, __ldcg(c.prefix_len + cache_list(i)));      // it never is less, nor may it be
             counts[i] = n;
-            lengths[i] = (n.x - shared_rows(i) + kAttnTileRows - 1) / kAttnTileRows + ((kBeside ? c.window : min(n.y, c.window)) + kAttnTileRows - 1) / kAttnTileRows;
+            lengths[i] = (n.x + kAttnTileRows - 1) / kAttnTileRows + ((kBeside ? c.window : min(n.y, c.window)) + kAttnTileRows - 1) / kAttnTileRows;
         }
         __syncthreads();
         // One wave: beside the step, on the SMs that it leaves, if what that adds to the wave's time is less than the step's;
@@ -441,13 +452,11 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         }
         n_parts = attn_unit(lengths, n_lists, n_units, blockIdx.x, lane, list, part);
         if (n_parts == 0) {                                        // the whole CTA: more CTAs than parts
-            if (!kShared) griddep_wait();
+            griddep_wait();
             return;
         }
         n_before = n_prefix = counts[list].x;
         n_total = counts[list].y;
-        n_shared = shared_rows(list);
-        if constexpr (kShared) look_up_group(list);
         if (kBeside && !beside) n_prefix = __ldcg(c.prefix_len + cache_list(list));
         fence_proxy_async_smem();                                  // the copies below write where these were read
         __syncthreads();
@@ -574,20 +583,20 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         if constexpr (kBeside) {
             int32_t t[kAttnStages + 1], page[kAttnStages + 1];
 #pragma unroll
-            for (int i = 0; i <= kAttnStages; ++i) t[i] = s_issue + i * kAttnWarps < n_tiles ? tile_at(s_issue + i * kAttnWarps) : -1;
+            for (int i = 0; i <= kAttnStages; ++i) t[i] = s_issue + i * kStep < n_tiles ? tile_at(s_issue + i * kStep) : -1;
 #pragma unroll
             for (int i = 0; i <= kAttnStages; ++i) page[i] = page_of(t[i]);
 #pragma unroll
             for (int i = 0; i <= kAttnStages; ++i) rows[i] = row_of(t[i], page[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i <= kAttnStages; ++i) rows[i] = s_issue + i * kAttnWarps < n_tiles ? tile_row(s_issue + i * kAttnWarps) : 0;
+            for (int i = 0; i <= kAttnStages; ++i) rows[i] = s_issue + i * kStep < n_tiles ? tile_row(s_issue + i * kStep) : 0;
         }
 #pragma unroll
         for (int i = 0; i < kAttnStages; ++i)
             if (s_issue < n_tiles) {
                 if (lane == 0) issue(s_issue, rows[i], (first_stage + i) % kAttnStages);
-                s_issue += kAttnWarps;
+                s_issue += kStep;
             }
         row_next = rows[kAttnStages];
     };
@@ -706,7 +715,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     };
     for (;;) {
     // no copies of this warp are in flight here
-    if (again) s = s_issue = s_first + warp;
+    if (again) s = s_issue = s_first + (kShared ? 0 : warp);
     if (!kFp8 && again) take_query();      // on their way beside the page numbers
     fill(stage);
     if (again) {
@@ -719,7 +728,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         l_run = vref = 0.0f;
         again = false;
     }
-    for (; s < n_tiles; s += kAttnWarps) {
+    for (; s < n_tiles; s += kStep) {
         if (kBeside && !waited && s_issue < n_tiles &&
             (s_issue + kAttnWarps >= n_tiles ||
              (p.n_parts == 0 && static_cast<uint32_t>(clock()) - started > static_cast<uint32_t>(kWaitBase + (kFp8 ? kWaitTile8 : kWaitTile) * kD / 128 * n_early)))) {
@@ -899,7 +908,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         __syncwarp();                                     // all lanes are done with this stage
         if (s_issue < n_tiles) {
             if (lane == 0) issue(s_issue, row_next, stage);
-            s_issue += kAttnWarps;
+            s_issue += kStep;
             row_next = s_issue < n_tiles ? tile_row(s_issue) : 0;
         }
         if (++stage == kAttnStages) { stage = 0; parity ^= 1u; }
@@ -937,6 +946,101 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             }
         }
     }
+    constexpr int kUnit = 16 + kAttnMaxGroup * kD;
+    if constexpr (kShared) {
+        // The warp's own part, or all parts of the list if it is the last of them to arrive, and what shared_attn_kernel has left of the list's shared
+        // rows.  Four elements of a query head a lane at a time, kItems of them side by side: their loads are one round trip.
+        __syncwarp();
+        const bool failed = *abort_flag != 0;
+        const float *own = reinterpret_cast<const float *>(smem + warp * kAttnStages * kStageBytes);
+        const int n_items = p.group * (kD / 4);
+        float *units = p.part_scratch + static_cast<int64_t>(long_unit0) * kUnit;
+        if (n_parts > 1) {
+            float *unit = units + static_cast<int64_t>(part) * kUnit;
+            for (int idx = lane; idx < n_items; idx += 32) {
+                const int gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                __stcg(reinterpret_cast<float4 *>(unit + 16 + gq * kD + d), *reinterpret_cast<const float4 *>(own + 16 + gq * kD + d));
+                if (d == 0) {
+                    __stcg(unit + gq, failed ? -INFINITY : own[gq]);
+                    __stcg(unit + 8 + gq, failed ? 0.0f : own[8 + gq]);
+                }
+            }
+            if (!arrive_last_warp(p.part_arrive + long_unit0, static_cast<uint32_t>(n_parts))) return;
+        }
+        griddep_wait();
+        constexpr int kItems = 4, kPieces = 4;
+        auto add = [](float &m, float &den, float4 &num, float m2, float l2, const float4 &o2) {
+            if (!(m2 > -INFINITY)) return;                         // nothing in it
+            const float m_new = fmaxf(m, m2), f = m > -INFINITY ? fast_ex2(m - m_new) : 0.0f, f2 = fast_ex2(m2 - m_new);
+            num.x *= f; num.y *= f; num.z *= f; num.w *= f;
+            attn_add(num, o2, f2);
+            den = den * f + l2 * f2;
+            m = m_new;
+        };
+        for (int idx0 = lane; idx0 < n_items; idx0 += 32 * kItems) {
+            float m[kItems], den[kItems];
+            float4 num[kItems];
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) {
+                const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                m[k] = own[gq];
+                den[k] = failed ? -INFINITY : own[8 + gq];
+                num[k] = *reinterpret_cast<const float4 *>(own + 16 + gq * kD + d);
+                if (n_parts > 1) { m[k] = -INFINITY; den[k] = 0.0f; num[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+            }
+            for (int i = 0; n_parts > 1 && i < n_parts; ++i) {     // in part order
+                const float *u = units + static_cast<int64_t>(i) * kUnit;
+                float m2[kItems], l2[kItems];
+                float4 o2[kItems];
+#pragma unroll
+                for (int k = 0; k < kItems; ++k) {
+                    const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                    m2[k] = __ldcg(u + gq);
+                    l2[k] = __ldcg(u + 8 + gq);
+                    o2[k] = __ldcg(reinterpret_cast<const float4 *>(u + 16 + gq * kD + d));
+                }
+#pragma unroll
+                for (int k = 0; k < kItems; ++k) add(m[k], den[k], num[k], m2[k], l2[k], o2[k]);
+            }
+            const float *o_at[kItems];                             // in the first slot
+            const float2 *ml_at[kItems];
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) {
+                const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                o_at[k] = p.share.part + share_part_at<kD>(sh_slot, p.share.rows_max, sh_row + gq, d);
+                ml_at[k] = p.share.part_ml + static_cast<int64_t>(sh_slot) * p.share.rows_max + sh_row + gq;
+            }
+#pragma unroll 1
+            for (int i0 = 0; i0 < sh_n; i0 += kPieces) {
+                float2 ml[kPieces][kItems];
+                float4 o2[kPieces][kItems];
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) {
+                    const int64_t on = static_cast<int64_t>(min(i0 + j, sh_n - 1)) * p.share.rows_max;
+#pragma unroll
+                    for (int k = 0; k < kItems; ++k) {
+                        ml[j][k] = __ldcg(ml_at[k] + on);
+                        o2[j][k] = __ldcg(reinterpret_cast<const float4 *>(o_at[k] + on * kD));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) {
+                    const bool in = i0 + j < sh_n;
+#pragma unroll
+                    for (int k = 0; k < kItems; ++k) {
+                        if (ml[j][k].y < 0.0f) den[k] = -INFINITY;  // a wait ran out there: zeros
+                        add(m[k], den[k], num[k], in ? ml[j][k].x : -INFINITY, ml[j][k].y, o2[j][k]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) {
+                const int idx = idx0 + 32 * k, gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                if (idx < n_items) attn_store(p.out + (row0 + gq) * kD + d, num[k], den[k]);      // an empty list gives zeros
+            }
+        }
+        return;
+    }
     __syncthreads();
     const bool failed = *abort_flag != 0;
     const int64_t out_row0 = kBeside ? query_row() : row0;
@@ -945,41 +1049,10 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         part = kept_s[warp][kPart];
         n_parts = kept_s[warp][kParts];
     }
-    constexpr int kUnit = 16 + kAttnMaxGroup * kD;
     // the list's first unit
     const int unit0 = p.n_parts == 0 ? static_cast<int>(blockIdx.x) - part
-                      : kShared ? long_unit0
                       : list >= p.head_lists ? p.tail_unit0 + (list - p.head_lists) * p.tail_parts : list * p.n_parts;
     float *unit = n_parts > 1 ? p.part_scratch + static_cast<int64_t>(unit0 + part) * kUnit : nullptr;
-    // kShared: what shared_attn_kernel has left of the list's shared rows, added to four elements of one query head
-    auto join_shared = [&](int gq, int d, float &m_all, float &den, float4 &num) {
-        constexpr int kPieces = 6;
-        for (int i0 = 0; i0 < sh_n; i0 += kPieces) {
-            float2 ml[kPieces];
-            float4 nv[kPieces];
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                const int64_t slot = static_cast<int64_t>(sh_slot) + i0 + j;
-                const bool in = i0 + j < sh_n;
-                ml[j] = in ? __ldcg(p.share.part_ml + slot * p.share.rows_max + sh_row + gq) : make_float2(-INFINITY, 0.0f);
-                nv[j] = in ? __ldcg(reinterpret_cast<const float4 *>(p.share.part + share_part_at<kD>(slot, p.share.rows_max, sh_row + gq, d)))
-                           : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                if (ml[j].y < 0.0f) den = -INFINITY;                    // a wait ran out there: zeros
-                if (!(ml[j].x > -INFINITY)) continue;
-                const float m_new = fmaxf(m_all, ml[j].x), f = m_all > -INFINITY ? fast_ex2(m_all - m_new) : 0.0f, g2 = fast_ex2(ml[j].x - m_new);
-                num.x *= f; num.y *= f; num.z *= f; num.w *= f;
-                attn_add(num, nv[j], g2);
-                den = den * f + ml[j].y * g2;
-                m_all = m_new;
-            }
-        }
-    };
-    if constexpr (kShared) {
-        if (n_parts == 1) griddep_wait();
-    }
     // four elements of one query head per thread
     for (int idx = threadIdx.x; idx < p.group * (kD / 4); idx += kAttnThreads) {
         const int gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
@@ -999,7 +1072,6 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
             }
         }
         if (n_parts == 1) {
-            if constexpr (kShared) join_shared(gq, d, m_all, den, num);
             attn_store(p.out + (out_row0 + gq) * kD + d, num, failed ? 0.0f : den);      // an empty list gives zeros
         } else {
             __stcg(reinterpret_cast<float4 *>(unit + 16 + gq * kD + d), num);
@@ -1014,10 +1086,9 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     // ---- several CTAs per list: the one that arrives last merges all parts, in part order
     __shared__ int last_s;
     __syncthreads();
-    if (threadIdx.x == 0) last_s = arrive_last(p.part_arrive + (kShared && p.n_parts > 0 ? long_unit0 : list - p.list0), static_cast<uint32_t>(n_parts));
+    if (threadIdx.x == 0) last_s = arrive_last(p.part_arrive + (list - p.list0), static_cast<uint32_t>(n_parts));
     __syncthreads();
     if (!last_s) return;
-    if constexpr (kShared) griddep_wait();
     const float *units = p.part_scratch + static_cast<int64_t>(unit0) * kUnit;
     constexpr int kBatch = 8;               // parts whose values are loaded together: one round trip to memory
     for (int idx = threadIdx.x; idx < p.group * (kD / 4); idx += kAttnThreads) {
@@ -1051,7 +1122,6 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
                 den += dv[j] * f;
             }
         }
-        if constexpr (kShared) join_shared(gq, d, m_all, den, num);
         attn_store(p.out + (out_row0 + gq) * kD + d, num, den);
     }
 }

@@ -3087,12 +3087,14 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
     }
     int64_t n_ctas = n_lists_call;
     p.n_parts = 1;
-    if (n_lists_call < slots && n_lists_call <= 32 * kAttnListsPerLane) {
+    if (share) {
+        // a warp per list, and for the further parts of long ones a wave of CTAs, or as many as there are lists
+        p.extra0 = static_cast<int32_t>(n_lists_call);
+        n_ctas = (n_lists_call + kAttnWarps - 1) / kAttnWarps;
+        n_ctas += std::min(std::max(slots, n_ctas), cache->attn_units / (2 * kAttnWarps));      // (scratch: at most two units for each of them)
+    } else if (n_lists_call < slots && n_lists_call <= 32 * kAttnListsPerLane) {
         p.n_parts = 0;
         n_ctas = slots;
-    } else if (share) {
-        p.extra0 = static_cast<int32_t>(n_lists_call);          // a CTA per list, and a wave of others for long ones (attn_long)
-        n_ctas = n_lists_call + slots;
     } else {
         const int64_t longest = static_cast<int64_t>(v.max_pages) * v.page_tokens + v.window;
         int64_t parts = static_cast<int64_t>(ctx->sm_count) * 24 / n_lists_call;
