@@ -951,92 +951,130 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         // The warp's own part, or all parts of the list if it is the last of them to arrive, and what shared_attn_kernel has left of the list's shared
         // rows.  Four elements of a query head a lane at a time, kItems of them side by side: their loads are one round trip.
         __syncwarp();
-        const bool failed = *abort_flag != 0;
-        const float *own = reinterpret_cast<const float *>(smem + warp * kAttnStages * kStageBytes);
+        bool failed = *abort_flag != 0;
+        float *own = reinterpret_cast<float *>(smem + warp * kAttnStages * kStageBytes);       // { m[8], l[8], O[8][kD] }, then weights [pieces][8]
         const int n_items = p.group * (kD / 4);
-        float *units = p.part_scratch + static_cast<int64_t>(long_unit0) * kUnit;
+        constexpr int kItems = 4, kPieces = 4;
         if (n_parts > 1) {
+            float *units = p.part_scratch + static_cast<int64_t>(long_unit0) * kUnit;
             float *unit = units + static_cast<int64_t>(part) * kUnit;
             for (int idx = lane; idx < n_items; idx += 32) {
                 const int gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
                 __stcg(reinterpret_cast<float4 *>(unit + 16 + gq * kD + d), *reinterpret_cast<const float4 *>(own + 16 + gq * kD + d));
                 if (d == 0) {
                     __stcg(unit + gq, failed ? -INFINITY : own[gq]);
-                    __stcg(unit + 8 + gq, failed ? 0.0f : own[8 + gq]);
+                    __stcg(unit + 8 + gq, failed ? -1.0f : own[8 + gq]);
                 }
             }
             if (!arrive_last_warp(p.part_arrive + long_unit0, static_cast<uint32_t>(n_parts))) return;
+            for (int idx = lane; idx < n_items; idx += 32) {           // in part order, to where the warp's own part was
+                const int gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
+                float m = -INFINITY, den = 0.0f;
+                float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int i0 = 0; i0 < n_parts; i0 += kPieces) {
+                    float mv[kPieces], dv[kPieces];
+                    float4 nv[kPieces];
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) {
+                        const float *u = units + static_cast<int64_t>(min(i0 + j, n_parts - 1)) * kUnit;
+                        mv[j] = i0 + j < n_parts ? __ldcg(u + gq) : -INFINITY;
+                        dv[j] = __ldcg(u + 8 + gq);
+                        nv[j] = __ldcg(reinterpret_cast<const float4 *>(u + 16 + gq * kD + d));
+                    }
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) {
+                        failed |= dv[j] < 0.0f;
+                        if (!(mv[j] > -INFINITY)) continue;             // nothing in it
+                        const float m_new = fmaxf(m, mv[j]), f = m > -INFINITY ? fast_ex2(m - m_new) : 0.0f, f2 = fast_ex2(mv[j] - m_new);
+                        num.x *= f; num.y *= f; num.z *= f; num.w *= f;
+                        attn_add(num, nv[j], f2);
+                        den = den * f + dv[j] * f2;
+                        m = m_new;
+                    }
+                }
+                *reinterpret_cast<float4 *>(own + 16 + gq * kD + d) = num;
+                if (d == 0) { own[gq] = m; own[8 + gq] = den; }
+            }
+            __syncwarp();
         }
         griddep_wait();
-        constexpr int kItems = 4, kPieces = 4;
-        auto add = [](float &m, float &den, float4 &num, float m2, float l2, const float4 &o2) {
-            if (!(m2 > -INFINITY)) return;                         // nothing in it
-            const float m_new = fmaxf(m, m2), f = m > -INFINITY ? fast_ex2(m - m_new) : 0.0f, f2 = fast_ex2(m2 - m_new);
-            num.x *= f; num.y *= f; num.z *= f; num.w *= f;
-            attn_add(num, o2, f2);
-            den = den * f + l2 * f2;
-            m = m_new;
+        float4 o2[kPieces][kItems];
+        const float *o_at[kItems];                                     // items idx0, idx0 + 32, ... in the first slot
+        auto places = [&](int idx0) {
+#pragma unroll
+            for (int k = 0; k < kItems; ++k) {
+                const int idx = min(idx0 + 32 * k, n_items - 1);
+                o_at[k] = p.share.part + share_part_at<kD>(sh_slot, p.share.rows_max, sh_row + idx / (kD / 4), idx % (kD / 4) * 4);
+            }
         };
+        auto load = [&](int i0) {                                      // of pieces i0, i0 + 1, ...
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int64_t on = static_cast<int64_t>(min(i0 + j, sh_n - 1)) * p.share.rows_max * kD;
+#pragma unroll
+                for (int k = 0; k < kItems; ++k) o2[j][k] = __ldcg(reinterpret_cast<const float4 *>(o_at[k] + on));
+            }
+        };
+        places(lane);
+        if (sh_n > 0) load(0);                                         // on their way beside what they weigh
+        // (m, l) of all pieces first, a lane for each of eight heads and four pieces at a time: what each piece weighs, worked out once
+        const int gq_l = lane & 7, j_l = lane >> 3;
+        const bool head = gq_l < p.group;
+        const float m_own = head ? own[gq_l] : -INFINITY, l_own = head ? own[8 + gq_l] : 0.0f;
+        float *weight = own + kUnit;
+        static_assert(kFp8 || kUnit * 4 + kShMostCtas * 32 <= kAttnStages * static_cast<int>(kStageBytes), "room for the weights");
+        const float2 *ml_at = p.share.part_ml + static_cast<int64_t>(sh_slot) * p.share.rows_max + sh_row + (head ? gq_l : 0);
+        float m = j_l == 0 ? m_own : -INFINITY, l = j_l == 0 ? l_own : 0.0f;
+        for (int i = j_l; i < sh_n; i += 4) {
+            const float2 ml = __ldcg(ml_at + static_cast<int64_t>(i) * p.share.rows_max);
+            failed |= ml.y < 0.0f;                                     // a wait ran out there: zeros
+            weight[i * 8 + gq_l] = ml.x;
+            const float m_new = fmaxf(m, ml.x);
+            if (m_new > -INFINITY) {
+                l = l * fast_ex2(m - m_new) + ml.y * fast_ex2(ml.x - m_new);
+                m = m_new;
+            }
+        }
+#pragma unroll
+        for (int o = 8; o <= 16; o <<= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o), m_new = fmaxf(m, m2);
+            if (m_new > -INFINITY) {
+                l = l * fast_ex2(m - m_new) + l2 * fast_ex2(m2 - m_new);
+                m = m_new;
+            }
+        }
+        failed = __any_sync(0xffffffffu, failed);
+        for (int i = j_l; i < sh_n; i += 4) weight[i * 8 + gq_l] = m > -INFINITY ? fast_ex2(weight[i * 8 + gq_l] - m) : 0.0f;
+        __syncwarp();                                                  // everybody has read own
+        if (lane < 8) {
+            own[lane] = m_own > -INFINITY ? fast_ex2(m_own - m) : 0.0f;
+            own[8 + lane] = failed ? 0.0f : l;
+        }
+        __syncwarp();
         for (int idx0 = lane; idx0 < n_items; idx0 += 32 * kItems) {
-            float m[kItems], den[kItems];
             float4 num[kItems];
+            int gq[kItems];
+            if (idx0 != lane) places(idx0);
 #pragma unroll
             for (int k = 0; k < kItems; ++k) {
-                const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
-                m[k] = own[gq];
-                den[k] = failed ? -INFINITY : own[8 + gq];
-                num[k] = *reinterpret_cast<const float4 *>(own + 16 + gq * kD + d);
-                if (n_parts > 1) { m[k] = -INFINITY; den[k] = 0.0f; num[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
-            }
-            for (int i = 0; n_parts > 1 && i < n_parts; ++i) {     // in part order
-                const float *u = units + static_cast<int64_t>(i) * kUnit;
-                float m2[kItems], l2[kItems];
-                float4 o2[kItems];
-#pragma unroll
-                for (int k = 0; k < kItems; ++k) {
-                    const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
-                    m2[k] = __ldcg(u + gq);
-                    l2[k] = __ldcg(u + 8 + gq);
-                    o2[k] = __ldcg(reinterpret_cast<const float4 *>(u + 16 + gq * kD + d));
-                }
-#pragma unroll
-                for (int k = 0; k < kItems; ++k) add(m[k], den[k], num[k], m2[k], l2[k], o2[k]);
-            }
-            const float *o_at[kItems];                             // in the first slot
-            const float2 *ml_at[kItems];
-#pragma unroll
-            for (int k = 0; k < kItems; ++k) {
-                const int idx = min(idx0 + 32 * k, n_items - 1), gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
-                o_at[k] = p.share.part + share_part_at<kD>(sh_slot, p.share.rows_max, sh_row + gq, d);
-                ml_at[k] = p.share.part_ml + static_cast<int64_t>(sh_slot) * p.share.rows_max + sh_row + gq;
+                const int idx = min(idx0 + 32 * k, n_items - 1), d = idx % (kD / 4) * 4;
+                gq[k] = idx / (kD / 4);
+                num[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (own[gq[k]] > 0.0f) attn_add(num[k], *reinterpret_cast<const float4 *>(own + 16 + gq[k] * kD + d), own[gq[k]]);
             }
 #pragma unroll 1
             for (int i0 = 0; i0 < sh_n; i0 += kPieces) {
-                float2 ml[kPieces][kItems];
-                float4 o2[kPieces][kItems];
+                if (idx0 != lane || i0 > 0) load(i0);
 #pragma unroll
-                for (int j = 0; j < kPieces; ++j) {
-                    const int64_t on = static_cast<int64_t>(min(i0 + j, sh_n - 1)) * p.share.rows_max;
+                for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-                    for (int k = 0; k < kItems; ++k) {
-                        ml[j][k] = __ldcg(ml_at[k] + on);
-                        o2[j][k] = __ldcg(reinterpret_cast<const float4 *>(o_at[k] + on * kD));
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kPieces; ++j) {
-                    const bool in = i0 + j < sh_n;
-#pragma unroll
-                    for (int k = 0; k < kItems; ++k) {
-                        if (ml[j][k].y < 0.0f) den[k] = -INFINITY;  // a wait ran out there: zeros
-                        add(m[k], den[k], num[k], in ? ml[j][k].x : -INFINITY, ml[j][k].y, o2[j][k]);
-                    }
-                }
+                    for (int k = 0; k < kItems; ++k)
+                        if (i0 + j < sh_n) attn_add(num[k], o2[j][k], weight[(i0 + j) * 8 + gq[k]]);
             }
 #pragma unroll
             for (int k = 0; k < kItems; ++k) {
-                const int idx = idx0 + 32 * k, gq = idx / (kD / 4), d = idx % (kD / 4) * 4;
-                if (idx < n_items) attn_store(p.out + (row0 + gq) * kD + d, num[k], den[k]);      // an empty list gives zeros
+                const int idx = idx0 + 32 * k;
+                if (idx < n_items) attn_store(p.out + (row0 + gq[k]) * kD + idx % (kD / 4) * 4, num[k], own[8 + gq[k]]);      // an empty list gives zeros
             }
         }
         return;

@@ -3510,7 +3510,7 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
     p.v.lists = cache->share_lists;
     p.v.n_subs = cache->share_subs;
     p.v.rows_max = cache->share_rows_max;
-    p.v.n_ctas = ctx->sm_count;
+    p.v.n_ctas = std::min(ctx->sm_count, kShMostCtas);
     p.v.stamp_now = cache->share_meta;
     p.v.stamp = cache->share_stamp;
     p.group = n_q_heads / c.n_kv_heads;
@@ -3532,7 +3532,7 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
             ProfScope prof(ctx, KVZAP_KERNEL_ATTENTION, stream);
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attrs[2];
-            make_launch(&cfg, attrs, dim3(static_cast<unsigned>(ctx->sm_count)), dim3(kShThreads), sh_smem_bytes(c.head_dim), stream,
+            make_launch(&cfg, attrs, dim3(static_cast<unsigned>(p.v.n_ctas)), dim3(kShThreads), sh_smem_bytes(c.head_dim), stream,
                         !ctx->profiling, 1);
             KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, shared_kernel(c.head_dim), cache->tm_kshare, cache->tm_vshare, p));
         }

@@ -31,6 +31,7 @@
 
 namespace kvzap {
 
+constexpr int kShMostCtas = 148;             // CTAs of a launch, and pieces of a list, at most
 constexpr int kShTile = 128;                 // shared rows per tile, rows of Q per group of warps
 constexpr int kShProducers = 3;              // warps that issue copies
 constexpr int kShThreads = 384;              // 2 x 4 softmax warps, producers, products
