@@ -63,6 +63,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "decode_kernels.cuh"
 #include "ptx.cuh"
 #include "shared_attn_kernel.cuh"
@@ -100,7 +102,10 @@ struct AttnParams {
     int32_t tiles_shift;        // logarithm of the tiles per page, or -1
     int32_t beside_ctas;        // kBeside: CTAs [0, beside_ctas) run beside the step, as many as find room
     int32_t beside_tiles;       // n_parts == 0: with more tiles than this in all lists all CTAs wait for the step
-    ShareView share;            // kShared: what shared_attn_kernel, ahead of this launch, leaves of the lists' shared rows
+};
+// kShared
+struct AttnSharedParams : AttnParams {
+    ShareView share;            // what shared_attn_kernel, ahead of this launch, leaves of the lists' shared rows
 };
 
 // The lists of a call, of lengths[0 .. n) tiles, cut into at most n_units (>= n) parts: a list of t tiles has
@@ -294,7 +299,7 @@ template <int kD, bool kFp8, bool kBeside, bool kShared = false>
 __global__ void __launch_bounds__(kAttnThreads, kFp8 ? 4 : 3)
 decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_constant__ CUtensorMap tmap_vpool,
                    const __grid_constant__ CUtensorMap tmap_kring, const __grid_constant__ CUtensorMap tmap_vring,
-                   const AttnParams p)
+                   const std::conditional_t<kShared, AttnSharedParams, AttnParams> p)
 {
     constexpr int kHalves = kD / 64;
     constexpr int kStep = kShared ? 1 : kAttnWarps;                 // tiles from one of a warp's to its next
@@ -346,22 +351,28 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     auto cache_list = [&](int i) {          // list i of the call among the cache's lists
         return (static_cast<int64_t>((i / H) % B) * c.n_layers + p.layer0 + i / (H * B)) * H + i % H;
     };
-    const int32_t stamp = kShared ? __ldcg(p.share.stamp_now) : 0;
-    auto shared_rows = [&](int i) {         // the two loads go out together
-        const int32_t rows = kShared ? __ldcg(c.share_rows + cache_list(i)) : 0;
-        return stamp == p.share.stamp ? rows : 0;
+    int32_t stamp = 0;
+    if constexpr (kShared) stamp = __ldcg(p.share.stamp_now);
+    auto shared_rows = [&](int i) -> int32_t {         // the two loads go out together
+        if constexpr (kShared) {
+            const int32_t rows = __ldcg(p.share.share_rows + cache_list(i));
+            return stamp == p.share.stamp ? rows : 0;
+        }
+        return 0;
     };
     int32_t n_shared = 0;                   // kShared: of this list
     // ... its group, its place there, tiles ahead of the call and in it: looked up beside the lengths
     int sh_sub = 0, sh_row = 0;
     int32_t sh_base = 0, sh_end = 0;
     auto look_up_group = [&](int i) {
+        if constexpr (kShared) {
         const int b = (i / H) % B;
         const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
         sh_sub = __ldcg(p.share.seq_sub + b);
         sh_row = __ldcg(p.share.seq_pos + b) * p.group;
         sh_base = __ldcg(&lists[0].x);
         sh_end = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x);
+        }
     };
     if constexpr (kShared) {
         auto tiles_of = [&](int i) {
@@ -691,12 +702,14 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         sh_slot = static_cast<int>(unit);
     }
     auto find_shared = [&]() {
+        if constexpr (kShared) {
         if (n_shared == 0) return;
         const int64_t tiles = sh_end - sh_base;
         const int ctas = share_ctas(tiles, p.share.n_ctas);
         const int c0 = share_owner(tiles, ctas, sh_first - sh_base);
         sh_slot += c0;
         sh_n = share_owner(tiles, ctas, sh_last - sh_base - 1) - c0 + 1;
+        }
     };
     float o[kNTiles][4];
     float m_run = 0.0f, l_run = 0.0f;

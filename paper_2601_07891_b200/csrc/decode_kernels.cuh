@@ -36,6 +36,9 @@ struct CacheView {
     uint8_t *active;          // [n_seqs]
     // prefix_len before the last one-launch step behind an attention, for the attention beside it (see decode_attn_kernel)
     int32_t *before;          // [n_lists]
+};
+// ... and what only the kernels around forked sequences look at.
+struct SharingView : CacheView {
     int32_t *page_refs;       // [n_pages_pool] owners of a page beyond the first (see pages_kernels.cuh)
     int32_t *share_rows;      // [n_lists] leading rows that are read with the list's group (see shared_attn_kernel.cuh), 0: none
 };

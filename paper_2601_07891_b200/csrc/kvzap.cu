@@ -2518,7 +2518,7 @@ extern "C" kvzap_status kvzap_prune_prefill_noalloc(const void *K, const void *V
 // Paged output and the decode-time cache.
 struct kvzap_cache {
     kvzap_ctx *ctx = nullptr;
-    kvzap::CacheView v;
+    kvzap::SharingView v;
     float *scores = nullptr;        // [L][B][H] scratch when the caller does not want the scores
     int64_t n_lists = 0;
     int step_parity = 0;
@@ -2532,6 +2532,7 @@ struct kvzap_cache {
     float *attn_scratch = nullptr;       // partial results of lists that are split over several CTAs
     uint32_t *attn_arrive = nullptr;     // [attn_split_lists] arrival counts, zero between launches
     int64_t attn_units = 0;              // capacity of attn_scratch in (list, part) units
+    bool counted = false;                // pages may be shared: sequences were forked, or tables imported
     std::vector<char> empty;             // [n_seqs] slots that were released and have not been given anything since
     // groups whose shared rows are read together (kvzap_cache_share); host view, then device buffers
     int32_t share_subs = 0, share_q_heads = 0, share_rows_max = 0, share_stamp = 0;
@@ -2761,7 +2762,7 @@ kvzap_status kvzap_cache_create(kvzap_ctx *ctx, kvzap_cache **out, int32_t n_seq
     cache->ctx = ctx;
     cache->n_lists = static_cast<int64_t>(n_seqs) * c.n_layers * c.n_kv_heads;
     try { cache->empty.assign(static_cast<size_t>(n_seqs), 0); } catch (...) { delete cache; return fail(ctx, KVZAP_ERR_CUDA, "out of host memory"); }
-    CacheView &v = cache->v;
+    SharingView &v = cache->v;
     memset(&v, 0, sizeof v);
     v.n_seqs = n_seqs; v.n_layers = c.n_layers; v.n_heads = c.n_kv_heads; v.row_units = c.head_dim / 8;
     v.window = window; v.page_tokens = page_tokens; v.max_pages = max_pages_per_list; v.n_pages_pool = n_pages_pool;
@@ -2958,7 +2959,7 @@ static decltype(&decode_attn_kernel<128, false, false>) attn_kernel(int d_attn, 
                : (beside ? decode_attn_kernel<64, false, true> : decode_attn_kernel<64, false, false>);
 }
 
-static decltype(&decode_attn_kernel<128, false, false>) attn_shared_kernel(int d_attn)
+static decltype(&decode_attn_kernel<128, false, false, true>) attn_shared_kernel(int d_attn)
 {
     return d_attn == 128 ? decode_attn_kernel<128, false, false, true> : decode_attn_kernel<64, false, false, true>;
 }
@@ -2973,7 +2974,7 @@ static kvzap_status attention_check(kvzap_ctx *ctx, kvzap_cache *cache, int32_t 
                                     const void *Q, int32_t n_q_heads, float scale, void *O, bool fp8)
 {
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (layer_begin < 0 || layer_end > c.n_layers || layer_begin >= layer_end)
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "attention: layer range [%d, %d) invalid", layer_begin, layer_end);
     if (!Q || !O || !aligned16(Q) || !aligned16(O))
@@ -3039,13 +3040,13 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
     begin_op(ctx);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     DeviceGuard guard(c.device);
     const kvzap_status checked = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, fp8);
     if (checked != KVZAP_OK) return checked;
     // elements per row as the attention sees them: head_dim bf16 values, or head_dim * 2 - 16 E4M3 codes
     const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
-    AttnParams p;
+    AttnSharedParams p;                                     // all but the kernel behind a shared_attn_kernel take its first part
     memset(&p, 0, sizeof p);
     p.c = v;
     p.layer0 = layer_begin;
@@ -3132,8 +3133,11 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
         cudaLaunchAttribute attrs[2];
         make_launch(&cfg, attrs, dim3(static_cast<unsigned>(n_ctas)), dim3(kAttnThreads), attn_smem_bytes(d_attn, fp8), stream,
                     !ctx->profiling, 1);
-        KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, share ? attn_shared_kernel(d_attn) : attn_kernel(d_attn, fp8, beside), cache->tm_kpool, cache->tm_vpool, cache->tm_kring,
-                                           cache->tm_vring, p));
+        if (share)
+            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_shared_kernel(d_attn), cache->tm_kpool, cache->tm_vpool, cache->tm_kring, cache->tm_vring, p));
+        else
+            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_kernel(d_attn, fp8, beside), cache->tm_kpool, cache->tm_vpool, cache->tm_kring,
+                                               cache->tm_vring, static_cast<const AttnParams &>(p)));
     }
     ctx->launches += 1;
     ctx->beside += beside ? 1 : 0;
@@ -3192,7 +3196,7 @@ static kvzap_status release_slots(kvzap_cache *cache, const int32_t *slots, int 
     cudaLaunchAttribute attrs[2];
     make_launch(&cfg, attrs, dim3(static_cast<unsigned>(cache->v.n_layers * cache->v.n_heads), static_cast<unsigned>(m)), dim3(32), 0,
                 stream, !ctx->profiling, 1);
-    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, release_seqs_kernel, cache->v, list));
+    KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, release_seqs_kernel, cache->v, list, cache->counted ? 1 : 0));
     ctx->launches += 1;
     for (int i = 0; i < m; ++i) cache->empty[list.slot[i]] = 1;
     return share_leaders(cache, stream);
@@ -3258,6 +3262,7 @@ kvzap_status kvzap_cache_fork(kvzap_cache *cache, const int32_t *src, const int3
     }
     DeviceGuard guard(ctx->cfg.device);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n > 0) cache->counted = true;
     // all releases first: a kernel that hands pages back does not run beside one that takes them
     for (int i = 0; i < n; i += kSlotBatch) {
         st = release_slots(cache, dst + i, std::min(n - i, kSlotBatch), stream);
@@ -3311,7 +3316,7 @@ static kvzap_status pack_args(kvzap_cache *cache, const char *call, PackArgs *a,
                               const float *scores)
 {
     kvzap_ctx *ctx = cache->ctx;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (n < 1 || !seqs || !row_start || !n_tokens || capacity_rows < 0 || (capacity_rows > 0 && (!K || !V)) || !aligned16(K) || !aligned16(V))
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: seqs (host), n >= 1, row_start, n_tokens and 16-byte aligned K and V are required", call);
     const int64_t n_lists = static_cast<int64_t>(n) * v.n_layers * v.n_heads;
@@ -3384,7 +3389,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     kvzap_ctx *ctx = cache->ctx;
     begin_op(ctx);
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (n_groups < 0 || (n_groups > 0 && (!group_start || !seqs)))
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start and seqs (host), n_groups >= 0 are required");
     if (n_q_heads < c.n_kv_heads || n_q_heads % c.n_kv_heads != 0 || n_q_heads / c.n_kv_heads > kAttnMaxGroup)
@@ -3493,7 +3498,7 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
     if (cache->share_subs == 0) return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, false);
     begin_op(ctx);
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     DeviceGuard guard(c.device);
     kvzap_status st = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, false);
     if (st != KVZAP_OK) return st;
@@ -3513,6 +3518,7 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
     p.v.n_ctas = std::min(ctx->sm_count, kShMostCtas);
     p.v.stamp_now = cache->share_meta;
     p.v.stamp = cache->share_stamp;
+    p.v.share_rows = v.share_rows;
     p.group = n_q_heads / c.n_kv_heads;
     p.box_rows = cache->share_box;
     p.scale_log2e = scale * 1.4426950408889634f;
@@ -3560,7 +3566,7 @@ kvzap_status kvzap_cache_export(kvzap_cache *cache, int32_t seq, int32_t layer, 
 {
     if (!cache || !K_out || !V_out || !n_rows || capacity_rows < 0) return KVZAP_ERR_INVALID_ARG;
     begin_op(cache->ctx);
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (seq < 0 || seq >= v.n_seqs || layer < 0 || layer >= v.n_layers || head < 0 || head >= v.n_heads)
         return fail(cache->ctx, KVZAP_ERR_INVALID_ARG, "export: (seq, layer, head) out of range");
     DeviceGuard guard(cache->ctx->cfg.device);
@@ -3597,6 +3603,7 @@ kvzap_status kvzap_cache_import(kvzap_cache *cache, const int32_t *prefix_len, c
         KVZAP_CUDA(ctx, cudaGetLastError());
     }
     std::fill(cache->empty.begin(), cache->empty.end(), 0);
+    cache->counted = true;
     const kvzap_status st = share_leaders(cache, stream);
     if (st != KVZAP_OK) return st;
     KVZAP_CUDA(ctx, cudaStreamSynchronize(stream));
@@ -3626,7 +3633,7 @@ static kvzap_status append_chunk(kvzap_ctx *ctx, kvzap_cache *cache, int32_t lay
                                  int64_t n_tokens, float tau, cudaStream_t stream)
 {
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     ChunkSeqs by_value;
     by_value.n = n_seqs <= kMaxChunkSeqs ? n_seqs : 0;
     for (int i = 0; i < by_value.n; ++i) by_value.slot[i] = seqs[i];
@@ -3689,7 +3696,7 @@ kvzap_status kvzap_prefill_to_cache(kvzap_ctx *ctx, kvzap_cache *cache, int32_t 
     begin_op(ctx);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (layer < 0 || layer >= c.n_layers || seq < 0 || seq >= v.n_seqs)
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "prefill_to_cache: layer %d / seq %d out of range", layer, seq);
     kvzap_status st = check_common(ctx, n_tokens, 1, nullptr);
@@ -3721,7 +3728,7 @@ kvzap_status kvzap_prefill_to_cache_batch(kvzap_ctx *ctx, kvzap_cache *cache, in
     begin_op(ctx);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const kvzap_config &c = ctx->cfg;
-    const CacheView &v = cache->v;
+    const SharingView &v = cache->v;
     if (layer < 0 || layer >= c.n_layers) return fail(ctx, KVZAP_ERR_INVALID_ARG, "prefill_to_cache_batch: layer %d out of range", layer);
     if (!seq_ids || !cu_seqlens || n_seqs < 1)
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "prefill_to_cache_batch: seq_ids (host), cu_seqlens (device), n_seqs >= 1 are required");

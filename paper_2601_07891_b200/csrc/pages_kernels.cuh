@@ -20,8 +20,9 @@ struct SlotPairs { int32_t src[kSlotBatch], dst[kSlotBatch], first[kSlotBatch]; 
 
 // The pages of lists (seq, *, *), one warp each, go onto the stack of released pages, apart from those that other lists hold
 // too; the lists become empty.  Runs alone on the stream (it is the one kernel that adds to the stack).
+// counted = 0: no page of this cache was ever shared.
 __global__ void __launch_bounds__(32)
-release_seqs_kernel(const CacheView c, const __grid_constant__ SlotList seqs)
+release_seqs_kernel(const SharingView c, const __grid_constant__ SlotList seqs, int counted)
 {
     griddep_wait();              // and lets nothing start before it is done
     const int32_t seq = seqs.slot[blockIdx.y];
@@ -29,7 +30,13 @@ release_seqs_kernel(const CacheView c, const __grid_constant__ SlotList seqs)
     const int lane = threadIdx.x;
     const int32_t n_pages = (c.prefix_len[li] + c.page_tokens - 1) / c.page_tokens;
     const int32_t *table = c.page_table + li * c.max_pages;
-    for (int32_t i0 = 0; i0 < n_pages; i0 += 1024) {             // 32 pages a lane
+    if (!counted) {
+        int32_t base = 0;
+        if (lane == 0 && n_pages > 0) base = atomicAdd(c.free_top, n_pages);
+        base = __shfl_sync(0xffffffffu, base, 0);
+        for (int32_t i = lane; i < n_pages; i += 32) c.free_stack[base + i] = table[i];
+    }
+    for (int32_t i0 = 0; counted && i0 < n_pages; i0 += 1024) {  // 32 pages a lane
         uint32_t mine = 0u;
         constexpr int kBatch = 4;                                 // pages whose round trips to memory go side by side
         for (int j0 = 0; j0 < 32 && i0 + j0 * 32 < n_pages; j0 += kBatch) {
@@ -74,7 +81,7 @@ release_seqs_kernel(const CacheView c, const __grid_constant__ SlotList seqs)
 }
 
 // Owners of each page after an import: counted, then one less (none stays none).
-__global__ void __launch_bounds__(256) count_refs_kernel(const CacheView c)
+__global__ void __launch_bounds__(256) count_refs_kernel(const SharingView c)
 {
     const int64_t li = blockIdx.x;
     const int32_t n_pages = min((c.prefix_len[li] + c.page_tokens - 1) / c.page_tokens, c.max_pages);
@@ -83,7 +90,7 @@ __global__ void __launch_bounds__(256) count_refs_kernel(const CacheView c)
         if (page >= 0 && page < c.n_pages_pool) atomicAdd(c.page_refs + page, 1);
     }
 }
-__global__ void __launch_bounds__(256) count_refs_end_kernel(const CacheView c)
+__global__ void __launch_bounds__(256) count_refs_end_kernel(const SharingView c)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (i < c.n_pages_pool) c.page_refs[i] = max(c.page_refs[i] - 1, 0);
@@ -110,7 +117,7 @@ __device__ __forceinline__ void copy_units(uint4 *__restrict__ kd, uint4 *__rest
 // rows behind them into a page of the child's own, the window.  Bound by writing the windows.
 constexpr int kForkThreads = 256;
 __global__ void __launch_bounds__(kForkThreads)
-fork_kernel(const CacheView c, const __grid_constant__ SlotPairs pairs, int32_t *__restrict__ status)
+fork_kernel(const SharingView c, const __grid_constant__ SlotPairs pairs, int32_t *__restrict__ status)
 {
     griddep_wait();
     __shared__ int32_t page_s;
@@ -154,7 +161,7 @@ fork_kernel(const CacheView c, const __grid_constant__ SlotPairs pairs, int32_t 
 // [row_start[i], row_start[i + 1]), its paged rows first, then its window, oldest first.  Beside the rows: n_tokens[i] (tokens
 // appended so far, by which a window's slots go round) and the scores of the window's tokens, oldest first, zeros behind.
 struct PackArgs {
-    CacheView c;
+    SharingView c;
     uint4 *K, *V;                        // [capacity_rows][row_units]
     int64_t capacity_rows;
     int64_t *row_start;                  // [n_lists + 1]
@@ -210,7 +217,7 @@ pack_kernel(const PackArgs a, const __grid_constant__ SlotList seqs)
 {
     griddep_wait();
     extern __shared__ int64_t start_s[];                       // [n_lists + 1]
-    const CacheView &c = a.c;
+    const SharingView &c = a.c;
     const int n = a.n_lists, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (kOut) {
         cta_sums(start_s, n, [&](int i) {
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(32)
 unpack_pages_kernel(const PackArgs a, const __grid_constant__ SlotList seqs)
 {
     griddep_wait();
-    const CacheView &c = a.c;
+    const SharingView &c = a.c;
     const int i = blockIdx.x, lane = threadIdx.x;
     const int64_t li = pack_list(c, seqs, i);
     const int64_t rows = a.row_start[i + 1] - a.row_start[i];

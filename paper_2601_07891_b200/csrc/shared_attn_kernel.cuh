@@ -49,6 +49,7 @@ struct ShareView {
     // Groups told after this call was captured have another stamp: the call then reads every list by itself.
     const int32_t *stamp_now;
     int32_t stamp;
+    const int32_t *share_rows;
 };
 
 struct SharedAttnParams {
@@ -182,7 +183,7 @@ __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_g
 // their tables, whole pages only.  Members whose slot holds no sequence are left out.  rows of a member's list that are read
 // with the group go to c.share_rows; lists[unit].x is the number of tiles, for now.  Fewer rows than a tile are not worth a tile.
 __global__ void __launch_bounds__(32)
-share_count_kernel(const CacheView c, const int32_t *__restrict__ sub_start, const int32_t *__restrict__ sub_seqs, int n_subs,
+share_count_kernel(const SharingView c, const int32_t *__restrict__ sub_start, const int32_t *__restrict__ sub_seqs, int n_subs,
                    int4 *__restrict__ lists)
 {
     griddep_wait();
@@ -229,7 +230,7 @@ share_count_kernel(const CacheView c, const int32_t *__restrict__ sub_start, con
 
 // Members have left their groups: for each (layer, group, head) a list that still has the shared rows.
 __global__ void __launch_bounds__(32)
-share_leader_kernel(const CacheView c, const int32_t *__restrict__ sub_seqs, int n_subs, int4 *__restrict__ lists)
+share_leader_kernel(const SharingView c, const int32_t *__restrict__ sub_seqs, int n_subs, int4 *__restrict__ lists)
 {
     griddep_wait();
     const int unit = blockIdx.x, lane = threadIdx.x;
