@@ -2373,7 +2373,9 @@ kvzap_status kvzap_rotary(kvzap_ctx *ctx, const int32_t *positions, int64_t n_to
         heads += t.n_heads;
     }
     if (n_tokens == 0 || heads == 0) return KVZAP_OK;
-    if (!positions) return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: positions are required");
+    if (!positions || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "rotary: positions (4-byte aligned) are required");
+    if (n_tokens > 0x7fffffffLL) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: more than 2^31 - 1 tokens");
     if (any && !fast) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "rotary: beside 8-bit rows the other tensors are 16-byte aligned too");
     DeviceGuard guard(ctx->cfg.device);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
@@ -3319,6 +3321,8 @@ static kvzap_status pack_args(kvzap_cache *cache, const char *call, PackArgs *a,
     const SharingView &v = cache->v;
     if (n < 1 || !seqs || !row_start || !n_tokens || capacity_rows < 0 || (capacity_rows > 0 && (!K || !V)) || !aligned16(K) || !aligned16(V))
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: seqs (host), n >= 1, row_start, n_tokens and 16-byte aligned K and V are required", call);
+    if ((reinterpret_cast<uintptr_t>(row_start) & 7u) != 0 || ((reinterpret_cast<uintptr_t>(n_tokens) | reinterpret_cast<uintptr_t>(scores)) & 3u) != 0)
+        return fail(ctx, KVZAP_ERR_INVALID_ARG, "%s: row_start, n_tokens and the scores must be aligned to their elements", call);
     const int64_t n_lists = static_cast<int64_t>(n) * v.n_layers * v.n_heads;
     if (n > kSlotBatch || n_lists > kPackLists)
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "%s: more than %d sequences or %d lists in one call", call, kSlotBatch, kPackLists);

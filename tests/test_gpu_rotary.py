@@ -266,6 +266,12 @@ def test_refusals(binding, ctx):
         r = binding.KvzapRows(*[row[f] for f, _ in binding.KvzapRows._fields_])
         return binding.load().kvzap_rotary(fresh.handle, positions.data_ptr(), 4, (binding.KvzapRows * 4)(r, r, r, r), n, 0, None)
 
+    lib = binding.load()
+    row = binding.rotary_rows(x, x, True)
+    assert lib.kvzap_rotary(fresh.handle, positions.data_ptr() + 2, 4, (binding.KvzapRows * 1)(row), 1, 0, None) == 1
+    assert lib.kvzap_rotary(fresh.handle, None, 4, (binding.KvzapRows * 1)(row), 1, 0, None) == 1
+    assert lib.kvzap_rotary(fresh.handle, positions.data_ptr(), -1, (binding.KvzapRows * 1)(row), 1, 0, None) == 1
+    assert lib.kvzap_rotary(fresh.handle, positions.data_ptr(), 1 << 31, (binding.KvzapRows * 1)(row), 1, 0, None) == 2
     other = torch.zeros(4, 2, 144, dtype=torch.uint8, device="cuda").data_ptr()
     assert status(n=0) == 1 and status(n=4) == 1
     assert status(n_heads=-1) == 1 and status(flags=4) == 1 and status(in_=None) == 1 and status(out=None) == 1

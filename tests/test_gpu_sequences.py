@@ -476,6 +476,8 @@ def test_refusals(binding):
     lib = binding.load()
     odd = K.data_ptr() + 2
     assert lib.kvzap_cache_pack(cache.handle, binding._ints([0]), 1, odd, odd, 4, start.data_ptr(), tokens.data_ptr(), None, None) == 1
+    assert lib.kvzap_cache_pack(cache.handle, binding._ints([0]), 1, K.data_ptr(), K.data_ptr(), 4, start.data_ptr() + 4, tokens.data_ptr(), None, None) == 1
+    assert lib.kvzap_cache_pack(cache.handle, binding._ints([0]), 1, K.data_ptr(), K.data_ptr(), 4, start.data_ptr(), tokens.data_ptr() + 2, None, None) == 1
     assert lib.kvzap_cache_fork(cache.handle, None, None, 1, None) == 1
     assert lib.kvzap_cache_fork(cache.handle, None, None, -1, None) == 1
     for args in ((K[:, :4], K, start, tokens, scores), (K, K, start[:2], tokens, scores), (K, K, start, tokens.float(), scores),

@@ -415,3 +415,86 @@ def test_refusals(binding):
     for kw in (dict(D=72, w=16, page=16), dict(D=128, w=8, page=16), dict(D=128, w=16, page=24)):
         other = Setup(binding, 2, 1, 2, kw["D"], kw["w"], kw["page"], 20)
         refused(lambda: other.cache.share([[0, 1]], 8), 2, "multiples")
+
+
+@pytest.mark.parametrize("hidden,grouped", [(128, False), (128, True), (0, True)])
+def test_forks_between_steps_that_overlap(binding, hidden, grouped):
+    """A context that trusts its producers, step and attention layer by layer: the attention beside a step, and the step beside an attention, find what a
+    fork, a release and an unpack have put in their place."""
+    from paper_2601_07891_b200 import synth
+    B, L, H, G, D, w = 5, 2, 8, 4, 128, 16
+    ctx = binding.Kvzap(256, hidden, H, D, L, max_tokens=128, trusted_producers=True)
+    for l in range(L):
+        wts = synth.mlp_weights(256, hidden, H, 3 + l, "cpu", 0.3) if hidden else synth.linear_weights(256, H, 3 + l, "cpu", 0.3)
+        ctx.set_weights(l, *[x.cuda() for x in wts])
+    pool = torch.full((2, 4000, 16, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    cache = ctx.create_cache(B, w, 16, pool[0], pool[1], 100)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    n = [0] + [190 + 7 * i for i in range(L * H)]
+    start = torch.tensor(n).cumsum(0).cuda()
+    rows = int(start[-1])
+
+    def fill(b):
+        cache.unpack([b], normal(rows, D), normal(rows, D), start, torch.full((L * H,), 20, dtype=torch.int32, device="cuda"),
+                     torch.zeros(L * H, w, device="cuda"))
+
+    fill(0)
+    fill(3)
+    beside = binding.kvzap_beside_count(ctx.handle)
+    for change in (lambda: cache.fork([0, 0], [1, 2]), lambda: cache.release_seq(1), lambda: cache.fork([3], [1]), lambda: fill(2),
+                   lambda: cache.fork([2, 2, 2], [0, 1, 4])):
+        change()
+        if grouped:
+            cache.share([[0, 1, 2], [3, 4]], H * G)
+        for _ in range(6):
+            X, K, V, Q = normal(L, B, 256), normal(L, B, H, D), normal(L, B, H, D), normal(L, B, H * G, D)
+            O = torch.empty_like(Q)
+            torch.cuda.synchronize()
+            for l in range(L):
+                cache.decode_step(l, l + 1, X[l:l + 1], K[l:l + 1], V[l:l + 1], 0.0)
+                (cache.attention_shared if grouped else cache.attention)(l, l + 1, Q[l:l + 1], out=O[l:l + 1])
+        torch.cuda.synchronize()
+        assert ctx.poll_status() == 0
+        Kp, Vp, at, _, _ = cache.pack(list(range(B)))
+        Kp, Vp, at = Kp.double(), Vp.double(), at.tolist()
+        for l in range(L):
+            for b in range(B):
+                for h in range(H):
+                    j = (b * L + l) * H + h
+                    got = O[l, b, h * G:(h + 1) * G].double()
+                    if at[j] == at[j + 1]:
+                        assert bool((got == 0).all())
+                        continue
+                    p = torch.softmax(Q[l, b, h * G:(h + 1) * G].double() @ Kp[at[j]:at[j + 1]].t() * D ** -0.5, -1)
+                    want, A = p @ Vp[at[j]:at[j + 1]], p @ Vp[at[j]:at[j + 1]].abs()
+                    assert bool(((got - want).abs() <= want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10)).all()), (l, b, h)
+    if hidden and not grouped:
+        assert binding.kvzap_beside_count(ctx.handle) > beside
+
+
+def test_own_rows_of_all_lengths(binding):
+    """Members that have added nothing, a few rows and thousands: lists of one warp, of many, and more parts than stand by."""
+    H, G, D = 2, 4, 64
+    s = Setup(binding, 8, 1, H, D, 16, 16, 2700, n_pages=60000, seed=15)
+    s.fill(0, [160, 2000])
+    s.cache.fork([0] * 7, [1, 2, 3, 4, 5, 6, 7])
+    s.cache.share([list(range(8))], H * G)
+    s.check(H * G)
+    for b, n in ((1, 100), (2, 390), (3, 401), (4, 3000), (5, 40000)):
+        for at in range(0, n, 64):
+            m = min(64, n - at)
+            s.cache.prefill(0, b, torch.zeros(m, 64, dtype=torch.bfloat16, device="cuda"), s.normal(H, m, D), s.normal(H, m, D), MINUS_INF)
+    s.check(H * G)
+    s.check(H * G, spread=5.0)
+
+
+def test_many_long_own_lists(binding):
+    """More parts than the further CTAs take at the shortest length: it is doubled."""
+    B, H, L, D = 40, 8, 4, 64
+    s = Setup(binding, B, L, H, D, 0, 64, 40, n_pages=B * L * H * 24, seed=16)
+    for b in range(38):
+        s.fill(b, _ragged(L * H, 900, 1400, b))
+    s.cache.fork([0, 0], [38, 39])
+    s.cache.share([[0, 38, 39], list(range(1, 38))], H)
+    s.check(H)
