@@ -6,8 +6,8 @@
 //
 // The angle is kept as a fraction of a turn in 64-bit fixed point: step_i = f_i / 2 pi * 2^64, and position * step_i modulo
 // 2^64 is the fraction, exactly (whole turns drop out by themselves; what is off is the step, 2^-53 of it).  Its upper 32 bits, a
-// signed multiple of 2^-31 half turns, go to sincospif: an angle is off by 2^-32 turns + the rounding to fp32, at any position,
-// without a 64-bit sine and without a table of positions.
+// signed multiple of 2^-31 half turns, go to sincospif as far as fp32 holds them, and what that leaves is added by the first term of
+// the sines' series: an angle is off by 2^-32 turns at any position, without a 64-bit sine and without a table of positions.
 //
 // Bound by reading each row once and writing it once: 32768 tokens, 32 + 8 heads of 128, 671 MB, 108 us (6.2 TB/s).  A thread has 8 pairs (two
 // 16-byte pieces of a head) of one token, works their sines out once and goes over the token's heads, of all tensors of the call, with
@@ -50,9 +50,14 @@ struct RotaryParams {
 __device__ __forceinline__ void rotary_turn(uint64_t step, int32_t position, float magnitude, float sign, float &c, float &s)
 {
     const uint64_t turn = step * static_cast<uint64_t>(static_cast<int64_t>(position));
-    sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 4.656612873077393e-10f /* 2^-31 */, &s, &c);
-    c *= magnitude;
-    s *= magnitude * sign;
+    const int32_t half_turns = static_cast<int32_t>(turn >> 32);                       // times 2^-31
+    const float near = __int2float_rn(half_turns);
+    float s0, c0;
+    sincospif(near * 4.656612873077393e-10f /* 2^-31 */, &s0, &c0);
+    // what the rounding to 24 bits has left, at most 2^-25 half turns (a whole half turn, 2^31, is one past the integers)
+    const float rest = static_cast<float>(static_cast<int32_t>(static_cast<uint32_t>(half_turns) - static_cast<uint32_t>(__float2ll_rn(near)))) * 1.4629180792671596e-9f /* pi 2^-31 */;
+    c = (c0 - s0 * rest) * magnitude;
+    s = (s0 + c0 * rest) * (magnitude * sign);
 }
 // two fp32 -> E4M3 codes, lo in the low byte; values beyond the format's largest go to it
 __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi)
