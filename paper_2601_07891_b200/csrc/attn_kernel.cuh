@@ -366,12 +366,12 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     int32_t sh_base = 0, sh_end = 0;
     auto look_up_group = [&](int i) {
         if constexpr (kShared) {
-        const int b = (i / H) % B;
-        const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
-        sh_sub = __ldcg(p.share.seq_sub + b);
-        sh_row = __ldcg(p.share.seq_pos + b) * p.group;
-        sh_base = __ldcg(&lists[0].x);
-        sh_end = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x);
+            const int b = (i / H) % B;
+            const int4 *lists = p.share.lists + static_cast<int64_t>(p.layer0) * p.share.n_subs * H;
+            sh_sub = __ldcg(p.share.seq_sub + b);
+            sh_row = __ldcg(p.share.seq_pos + b) * p.group;
+            sh_base = __ldcg(&lists[0].x);
+            sh_end = __ldcg(&lists[static_cast<int64_t>(p.n_layers_call) * p.share.n_subs * H].x);
         }
     };
     if constexpr (kShared) {
@@ -703,12 +703,12 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
     }
     auto find_shared = [&]() {
         if constexpr (kShared) {
-        if (n_shared == 0) return;
-        const int64_t tiles = sh_end - sh_base;
-        const int ctas = share_ctas(tiles, p.share.n_ctas);
-        const int c0 = share_owner(tiles, ctas, sh_first - sh_base);
-        sh_slot += c0;
-        sh_n = share_owner(tiles, ctas, sh_last - sh_base - 1) - c0 + 1;
+            if (n_shared == 0) return;
+            const int64_t tiles = sh_end - sh_base;
+            const int ctas = share_ctas(tiles, p.share.n_ctas);
+            const int c0 = share_owner(tiles, ctas, sh_first - sh_base);
+            sh_slot += c0;
+            sh_n = share_owner(tiles, ctas, sh_last - sh_base - 1) - c0 + 1;
         }
     };
     float o[kNTiles][4];

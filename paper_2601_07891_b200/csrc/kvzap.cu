@@ -3400,7 +3400,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: n_q_heads must be 1..%d times the number of KV heads", kAttnMaxGroup);
     if ((c.head_dim != 64 && c.head_dim != 128) || v.page_tokens % kAttnTileRows != 0 || v.window % kAttnTileRows != 0)
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: head_dim 64 or 128, page_tokens and window multiples of %d are required", kAttnTileRows);
-    if (v.n_seqs >= 1 << 22) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: more than 2^22 sequences");
+    if (v.n_seqs >= 1 << 22 || cache->n_lists >= int64_t{1} << 31) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: 2^22 sequences or 2^31 lists, or more");
     int32_t n_members = 0;
     if (n_groups > 0) {
         if (group_start[0] != 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start begins with 0");

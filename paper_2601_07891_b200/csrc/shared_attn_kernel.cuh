@@ -402,118 +402,118 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const CacheView &c = p.c;
 
     if (warp >= 8) {
-    regs_fewer<kShRegsOthers>();          // the whole warpgroup, at this one place
-    if (warp < 8 + kShProducers) {
-        named_barrier_sync(4, 256 + 32 * kShProducers);       // the queries' loads are on their way: behind a ring full of rows they took 6 us
-        // ---- copies.  A tile is n_boxes x kHalves boxes, numbered with the halves fastest; lane i of producer q has number q + kShProducers i
-        const int n_boxes = kShTile / p.box_rows, mine = warp - 8 + kShProducers * lane;
-        const int box = mine / kHalves, half = mine % kHalves;
-        const uint64_t policy = l2_policy_evict_first();
-        const uint32_t box_bytes = p.box_rows * 128u;
-        while (ok && share_next(p, walk, x)) {
-            const int n = x.t1 - x.t0;
-            const int32_t *pages = c.page_table + static_cast<int64_t>(x.leader) * c.max_pages;
-            // of this lane's box of tile t: its page and its first row there (-1: no such box); the page number is on its way while the tiles
-            // before are copied
-            struct Place { int32_t page, row; };
-            auto place_of = [&](int t) -> Place {
-                const int32_t r = (x.t0 + t) * kShTile + box * p.box_rows;
-                if (t >= n || box >= n_boxes || r >= x.n_rows) return {0, -1};
-                const int32_t page_i = r / c.page_tokens;
-                return {__ldcg(pages + page_i), r - page_i * c.page_tokens};
-            };
-            auto copy = [&](const CUtensorMap *map, uint32_t pos, const Place &at) {
-                const uint32_t i = pos0 + pos, stage = i % kStages, round = i / kStages;
-                if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
-                const uint32_t who = __ballot_sync(0xffffffffu, at.row >= 0);
-                if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, __popc(who) * box_bytes);
-                __syncwarp();
-                if (at.row >= 0)
-                    tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * box_bytes, map, full + 8 * stage, half * 64,
-                                at.page * c.page_tokens + at.row, policy);
-            };
-            Place cur = place_of(0), next = place_of(1);
-            copy(&tmap_k, 0, cur);
-            for (int t = 0; ok && t < n; ++t) {
-                const Place after = place_of(t + 2);
-                if (t + 1 < n) copy(&tmap_k, sh_k_pos(t + 1), next);
-                if (ok) copy(&tmap_v, sh_v_pos(t, n), cur);
-                cur = next;
-                next = after;
-            }
-            pos0 += 2 * n;
-        }
-    } else {
-        // ---- matrix products: S of step i + 2 directly behind P V of step i, whose K has been waited for by then: the unit takes 850 cycles for S
-        // (128 bytes of operands a cycle from shared memory) and 640 for P V, and idles through every wait in between
-        const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
-        const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
-        uint32_t n_p[2] = {0u, 0u}, n_piece = 0;
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_s));
-            return ok;
-        };
-        while (ok && share_next(p, walk, x)) {
-            const int n = x.t1 - x.t0;
-            const bool two = x.n_mem * p.group > 128;
-            const int steps = two ? 2 * n : n;
-            if (!wait(q_full, n_piece & 1)) break;
-            if (n_piece > 0 && !wait(o_free, (n_piece - 1) & 1)) break;
-            auto tile_of = [&](int i) { return two ? i >> 1 : i; };
-            auto k_at = [&](int i) { return pos0 + sh_k_pos(tile_of(i)); };
-            auto k_full = [&](int i) { return wait(full + 8 * (k_at(i) % kStages), (k_at(i) / kStages) & 1); };
-            const uint64_t qd = uniform64(umma_desc_k_major_sw128(qtile));
-            auto scores = [&](int i) {                            // by one thread
-                const int w = i & 1;
-                const uint32_t stage = k_at(i) % kStages;
-                const uint64_t qw = qd + (two ? w * (kStageBytes >> 4) : 0u), kd = umma_desc_k_major_sw128(ring + stage * kStageBytes);
-#pragma unroll
-                for (int ks = 0; ks < kD / 16; ++ks) {
-                    const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32u) >> 4;
-                    umma_bf16(tmem + 256 * w, qw + off, kd + off, idesc_s, ks > 0);
+        regs_fewer<kShRegsOthers>();          // the whole warpgroup, at this one place
+        if (warp < 8 + kShProducers) {
+            named_barrier_sync(4, 256 + 32 * kShProducers);       // the queries' loads are on their way: behind a ring full of rows they took 6 us
+            // ---- copies.  A tile is n_boxes x kHalves boxes, numbered with the halves fastest; lane i of producer q has number q + kShProducers i
+            const int n_boxes = kShTile / p.box_rows, mine = warp - 8 + kShProducers * lane;
+            const int box = mine / kHalves, half = mine % kHalves;
+            const uint64_t policy = l2_policy_evict_first();
+            const uint32_t box_bytes = p.box_rows * 128u;
+            while (ok && share_next(p, walk, x)) {
+                const int n = x.t1 - x.t0;
+                const int32_t *pages = c.page_table + static_cast<int64_t>(x.leader) * c.max_pages;
+                // of this lane's box of tile t: its page and its first row there (-1: no such box); the page number is on its way while the tiles
+                // before are copied
+                struct Place { int32_t page, row; };
+                auto place_of = [&](int t) -> Place {
+                    const int32_t r = (x.t0 + t) * kShTile + box * p.box_rows;
+                    if (t >= n || box >= n_boxes || r >= x.n_rows) return {0, -1};
+                    const int32_t page_i = r / c.page_tokens;
+                    return {__ldcg(pages + page_i), r - page_i * c.page_tokens};
+                };
+                auto copy = [&](const CUtensorMap *map, uint32_t pos, const Place &at) {
+                    const uint32_t i = pos0 + pos, stage = i % kStages, round = i / kStages;
+                    if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
+                    const uint32_t who = __ballot_sync(0xffffffffu, at.row >= 0);
+                    if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, __popc(who) * box_bytes);
+                    __syncwarp();
+                    if (at.row >= 0)
+                        tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * box_bytes, map, full + 8 * stage, half * 64,
+                                    at.page * c.page_tokens + at.row, policy);
+                };
+                Place cur = place_of(0), next = place_of(1);
+                copy(&tmap_k, 0, cur);
+                for (int t = 0; ok && t < n; ++t) {
+                    const Place after = place_of(t + 2);
+                    if (t + 1 < n) copy(&tmap_k, sh_k_pos(t + 1), next);
+                    if (ok) copy(&tmap_v, sh_v_pos(t, n), cur);
+                    cur = next;
+                    next = after;
                 }
-                umma_commit(s_full + 8 * w);
-                if (!two || w == 1) umma_commit(empty + 8 * stage);
-            };
-            for (int i = 0; ok && i < min(steps, 2); ++i) {
-                if (!k_full(i)) break;
-                tc_fence_after_sync();
-                if (elect_one()) scores(i);
-                __syncwarp();
+                pos0 += 2 * n;
             }
-            for (int i = 0; ok && i < steps; ++i) {
-                const int t = tile_of(i), w = i & 1;
-                const uint32_t at = pos0 + sh_v_pos(t, n), stage = at % kStages;
-                const int groups = min(kShTile, x.n_rows - (x.t0 + t) * kShTile) / 16;      // rows of 16
-                const uint64_t vd = uniform64(umma_desc_n_major_sw128(ring + stage * kStageBytes, kHalfBytes));
-                const uint32_t to_s = uniform32(tmem + 256 * w);
-                if (!wait(full + 8 * stage, (at / kStages) & 1)) break;
+        } else {
+            // ---- matrix products: S of step i + 2 directly behind P V of step i, whose K has been waited for by then: the unit takes 850 cycles for S
+            // (128 bytes of operands a cycle from shared memory) and 640 for P V, and idles through every wait in between
+            const uint32_t idesc_s = umma_idesc_bf16_f32(128, kShTile);
+            const uint32_t idesc_o = umma_idesc_bf16_f32(128, kD) | kIdescBNMajor;
+            uint32_t n_p[2] = {0u, 0u}, n_piece = 0;
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, &abort_s));
+                return ok;
+            };
+            while (ok && share_next(p, walk, x)) {
+                const int n = x.t1 - x.t0;
+                const bool two = x.n_mem * p.group > 128;
+                const int steps = two ? 2 * n : n;
+                if (!wait(q_full, n_piece & 1)) break;
+                if (n_piece > 0 && !wait(o_free, (n_piece - 1) & 1)) break;
+                auto tile_of = [&](int i) { return two ? i >> 1 : i; };
+                auto k_at = [&](int i) { return pos0 + sh_k_pos(tile_of(i)); };
+                auto k_full = [&](int i) { return wait(full + 8 * (k_at(i) % kStages), (k_at(i) / kStages) & 1); };
+                const uint64_t qd = uniform64(umma_desc_k_major_sw128(qtile));
+                auto scores = [&](int i) {                            // by one thread
+                    const int w = i & 1;
+                    const uint32_t stage = k_at(i) % kStages;
+                    const uint64_t qw = qd + (two ? w * (kStageBytes >> 4) : 0u), kd = umma_desc_k_major_sw128(ring + stage * kStageBytes);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {            // as P comes
-                    if (half == 1 && i + 2 < steps && !k_full(i + 2)) break;
-                    if (!wait(p_full + 16 * w + 8 * half, n_p[w] & 1)) break;
-                    tc_fence_after_sync();
-                    const uint32_t more = uniform32(i > 1 || half > 0);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int ks = 4 * half + k;
-                            if (ks < groups) umma_bf16_ts(to_s + 128, to_s + 8 * ks, vd + ks * (2048u >> 4), idesc_o, k > 0 ? 1u : more);
-                        }
-                        if (half == 1) {
-                            if (!two || w == 1) umma_commit(empty + 8 * stage);
-                            if (i + 1 == steps) umma_commit(done);
-                            if (i + 2 < steps) scores(i + 2);
-                        }
+                    for (int ks = 0; ks < kD / 16; ++ks) {
+                        const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32u) >> 4;
+                        umma_bf16(tmem + 256 * w, qw + off, kd + off, idesc_s, ks > 0);
                     }
+                    umma_commit(s_full + 8 * w);
+                    if (!two || w == 1) umma_commit(empty + 8 * stage);
+                };
+                for (int i = 0; ok && i < min(steps, 2); ++i) {
+                    if (!k_full(i)) break;
+                    tc_fence_after_sync();
+                    if (elect_one()) scores(i);
                     __syncwarp();
                 }
-                n_p[w] += 1;
+                for (int i = 0; ok && i < steps; ++i) {
+                    const int t = tile_of(i), w = i & 1;
+                    const uint32_t at = pos0 + sh_v_pos(t, n), stage = at % kStages;
+                    const int groups = min(kShTile, x.n_rows - (x.t0 + t) * kShTile) / 16;      // rows of 16
+                    const uint64_t vd = uniform64(umma_desc_n_major_sw128(ring + stage * kStageBytes, kHalfBytes));
+                    const uint32_t to_s = uniform32(tmem + 256 * w);
+                    if (!wait(full + 8 * stage, (at / kStages) & 1)) break;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {            // as P comes
+                        if (half == 1 && i + 2 < steps && !k_full(i + 2)) break;
+                        if (!wait(p_full + 16 * w + 8 * half, n_p[w] & 1)) break;
+                        tc_fence_after_sync();
+                        const uint32_t more = uniform32(i > 1 || half > 0);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int ks = 4 * half + k;
+                                if (ks < groups) umma_bf16_ts(to_s + 128, to_s + 8 * ks, vd + ks * (2048u >> 4), idesc_o, k > 0 ? 1u : more);
+                            }
+                            if (half == 1) {
+                                if (!two || w == 1) umma_commit(empty + 8 * stage);
+                                if (i + 1 == steps) umma_commit(done);
+                                if (i + 2 < steps) scores(i + 2);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    n_p[w] += 1;
+                }
+                pos0 += 2 * n;
+                n_piece += 1;
             }
-            pos0 += 2 * n;
-            n_piece += 1;
         }
-    }
     } else {
         // ---- softmax: thread = row of Q
         regs_more<kShRegsSoftmax>();
