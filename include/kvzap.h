@@ -46,7 +46,7 @@
  *     Decoding layer by layer in this mode: enqueue kvzap_decode_attention directly behind kvzap_decode_step of
  *     the same layers, where the queries are there by then.  The attention then runs beside the step; with a
  *     kernel of the caller between the two (which is safe) it cannot, and takes a few microseconds longer.
- *   - Stream capture (CUDA graphs): kvzap_decode_step(_fp8), kvzap_decode_attention(_fp8), kvzap_decode_attention_shared
+ *   - Stream capture (CUDA graphs): kvzap_decode_step(_fp8), kvzap_decode_attention(_fp8), kvzap_decode_attention_shared(_fp8)
  *     and kvzap_rotary may be captured and replayed.  The other calls rotate scratch sets and counters on the host from call to call and must
  *     be enqueued, not captured.
  *   - Errors the host can see (bad argument, unsupported shape) return at once
@@ -571,7 +571,7 @@ kvzap_status kvzap_cache_unpack(kvzap_cache *cache, const int32_t *seqs, int32_t
  *   group_start [n_groups + 1], seqs int32, HOST (read before return); a slot is in one group at most, others are read by themselves
  *   n_q_heads: query heads of the attention calls to come (1..8 times the KV heads)
  * n_groups = 0 takes all groups back.  The first call allocates device memory (up to some 64 MB, or what one layer needs; more only
- * for larger groups), a later one may.  Same limits on D, pages and window as kvzap_decode_attention.
+ * for larger groups), a later one may.  Same limits on D, pages and window as kvzap_decode_attention and kvzap_decode_attention_fp8.
  */
 kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, const int32_t *seqs, int32_t n_groups,
                                int32_t n_q_heads, void *stream);
@@ -585,6 +585,10 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
  */
 kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
                                            const void *Q, int32_t n_q_heads, float scale, void *O, void *stream);
+
+/* The same over a cache of 8-bit rows: to kvzap_decode_attention_fp8 what the call above is to kvzap_decode_attention. */
+kvzap_status kvzap_decode_attention_shared_fp8(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,
+                                               const void *Q, int32_t n_q_heads, float scale, void *O, void *stream);
 
 /* lengths [n_seqs, L, H] int32 (device): rows currently held by each list (prefix + window). */
 kvzap_status kvzap_cache_lengths(kvzap_cache *cache, int32_t *lengths, void *stream);

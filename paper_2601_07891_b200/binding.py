@@ -99,6 +99,7 @@ SIGNATURES = {
     "kvzap_cache_unpack": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp]),
     "kvzap_cache_share": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp]),
     "kvzap_decode_attention_shared": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
+    "kvzap_decode_attention_shared_fp8": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_set_rotary": (_i32, [_vp, ctypes.POINTER(KvzapRotaryConfig)]),
     "kvzap_rotary": (_i32, [_vp, _vp, _i64, ctypes.POINTER(KvzapRows), _i32, _i32, _vp]),
     "kvzap_cache_lengths": (_i32, [_vp, _vp, _vp]),
@@ -432,6 +433,12 @@ def kvzap_decode_attention_shared(handle, cache, layer_begin, layer_end, Q, scal
     """Q, O [layer_end - layer_begin, n_seqs, n_q_heads, D] bf16 on the device."""
     _check(handle, load().kvzap_decode_attention_shared(handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O),
                                                         _stream(stream)))
+
+
+def kvzap_decode_attention_shared_fp8(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None):
+    """The same over 8-bit rows (see kvzap_decode_attention_fp8)."""
+    _check(handle, load().kvzap_decode_attention_shared_fp8(handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O),
+                                                            _stream(stream)))
 
 
 def kvzap_set_rotary(handle, head_dim, rotary_dim, base=10000.0, interleaved=False, factor=1.0, original_context=0.0, low=1.0,

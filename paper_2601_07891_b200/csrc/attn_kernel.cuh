@@ -1035,7 +1035,7 @@ decode_attn_kernel(const __grid_constant__ CUtensorMap tmap_kpool, const __grid_
         const bool head = gq_l < p.group;
         const float m_own = head ? own[gq_l] : -INFINITY, l_own = head ? own[8 + gq_l] : 0.0f;
         float *weight = own + kUnit;
-        static_assert(kFp8 || kUnit * 4 + kShMostCtas * 32 <= kAttnStages * static_cast<int>(kStageBytes), "room for the weights");
+        static_assert(kUnit * 4 + kShMostCtas * 32 <= kAttnStages * static_cast<int>(kStageBytes), "room for the weights");
         const float2 *ml_at = p.share.part_ml + static_cast<int64_t>(sh_slot) * p.share.rows_max + sh_row + (head ? gq_l : 0);
         float m = j_l == 0 ? m_own : -INFINITY, l = j_l == 0 ? l_own : 0.0f;
         for (int i = j_l; i < sh_n; i += 4) {

@@ -2961,14 +2961,16 @@ static decltype(&decode_attn_kernel<128, false, false>) attn_kernel(int d_attn, 
                : (beside ? decode_attn_kernel<64, false, true> : decode_attn_kernel<64, false, false>);
 }
 
-static decltype(&decode_attn_kernel<128, false, false, true>) attn_shared_kernel(int d_attn)
+static decltype(&decode_attn_kernel<128, false, false, true>) attn_shared_kernel(int d_attn, bool fp8)
 {
+    if (fp8) return d_attn == 128 ? decode_attn_kernel<128, true, false, true> : decode_attn_kernel<64, true, false, true>;
     return d_attn == 128 ? decode_attn_kernel<128, false, false, true> : decode_attn_kernel<64, false, false, true>;
 }
 
-static decltype(&shared_attn_kernel<128>) shared_kernel(int head_dim)
+static decltype(&shared_attn_kernel<128, false>) shared_kernel(int d_attn, bool fp8)
 {
-    return head_dim == 128 ? shared_attn_kernel<128> : shared_attn_kernel<64>;
+    if (fp8) return d_attn == 128 ? shared_attn_kernel<128, true> : shared_attn_kernel<64, true>;
+    return d_attn == 128 ? shared_attn_kernel<128, false> : shared_attn_kernel<64, false>;
 }
 
 // The checks of an attention call, and what its first one builds.
@@ -3018,7 +3020,7 @@ static kvzap_status attention_check(kvzap_ctx *ctx, kvzap_cache *cache, int32_t 
                 cudaError_t e = cudaSuccess;
                 for (int beside = 0; beside < 2 && e == cudaSuccess; ++beside)
                     e = cudaFuncSetAttribute(attn_kernel(d_attn, fp8, beside != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-                if (!fp8 && e == cudaSuccess) e = cudaFuncSetAttribute(attn_shared_kernel(d_attn), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+                if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_shared_kernel(d_attn, fp8), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
                 if (e == cudaSuccess) cache->attn_state = fp8 ? 2 : 1;
             }
         }
@@ -3136,7 +3138,7 @@ static kvzap_status attention_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t l
         make_launch(&cfg, attrs, dim3(static_cast<unsigned>(n_ctas)), dim3(kAttnThreads), attn_smem_bytes(d_attn, fp8), stream,
                     !ctx->profiling, 1);
         if (share)
-            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_shared_kernel(d_attn), cache->tm_kpool, cache->tm_vpool, cache->tm_kring, cache->tm_vring, p));
+            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_shared_kernel(d_attn, fp8), cache->tm_kpool, cache->tm_vpool, cache->tm_kring, cache->tm_vring, p));
         else
             KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, attn_kernel(d_attn, fp8, beside), cache->tm_kpool, cache->tm_vpool, cache->tm_kring,
                                                cache->tm_vring, static_cast<const AttnParams &>(p)));
@@ -3398,8 +3400,10 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start and seqs (host), n_groups >= 0 are required");
     if (n_q_heads < c.n_kv_heads || n_q_heads % c.n_kv_heads != 0 || n_q_heads / c.n_kv_heads > kAttnMaxGroup)
         return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: n_q_heads must be 1..%d times the number of KV heads", kAttnMaxGroup);
-    if ((c.head_dim != 64 && c.head_dim != 128) || v.page_tokens % kAttnTileRows != 0 || v.window % kAttnTileRows != 0)
-        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: head_dim 64 or 128, page_tokens and window multiples of %d are required", kAttnTileRows);
+    const bool fp8 = c.head_dim == 40 || c.head_dim == 72;      // rows of 64 or 128 codes
+    const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
+    if ((d_attn != 64 && d_attn != 128) || v.page_tokens % kAttnTileRows != 0 || v.window % kAttnTileRows != 0)
+        return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: head_dim 64 or 128 (8-bit rows: 40 or 72), page_tokens and window multiples of %d are required", kAttnTileRows);
     if (v.n_seqs >= 1 << 22 || cache->n_lists >= int64_t{1} << 31) return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: 2^22 sequences or 2^31 lists, or more");
     int32_t n_members = 0;
     if (n_groups > 0) {
@@ -3453,7 +3457,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     // Slots for the pieces that a launch leaves behind; a call of more layers than there is room for takes them in turns, so that what one launch
     // leaves is still in the L2 when the next one reads it.
     constexpr size_t kSlotsBytes = size_t{64} << 20;
-    const size_t slot_bytes = static_cast<size_t>(rows_max) * (sizeof(float) * c.head_dim + sizeof(float2));
+    const size_t slot_bytes = static_cast<size_t>(rows_max) * (sizeof(float) * d_attn + sizeof(float2));
     const size_t per_layer = static_cast<size_t>(n_subs) * c.n_kv_heads;
     size_t layers = kSlotsBytes / slot_bytes > static_cast<size_t>(ctx->sm_count) ? (kSlotsBytes / slot_bytes - ctx->sm_count) / per_layer : 0;
     layers = std::min(std::max(layers, size_t{1}), static_cast<size_t>(c.n_layers));
@@ -3471,11 +3475,18 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
         const uint64_t rows = static_cast<uint64_t>(v.n_pages_pool) * v.page_tokens;
         if (rows >= (uint64_t{1} << 31) || rows < static_cast<uint64_t>(box))
             return fail(ctx, KVZAP_ERR_UNSUPPORTED, "share: the pools must have fewer than 2^31 rows, and a page");
-        st = make_tmap(ctx, &cache->tm_kshare, v.k_pool, rows, c.head_dim, static_cast<uint32_t>(box));
-        if (st == KVZAP_OK) st = make_tmap(ctx, &cache->tm_vshare, v.v_pool, rows, c.head_dim, static_cast<uint32_t>(box));
+        if (fp8) {                                              // 16 whole rows, as decode_attn_kernel takes them
+            box = kAttnTileRows;
+            const uint32_t rb = static_cast<uint32_t>(c.head_dim) * 2;
+            st = make_tmap_rows(ctx, &cache->tm_kshare, v.k_pool, rows, rb, kAttnTileRows);
+            if (st == KVZAP_OK) st = make_tmap_rows(ctx, &cache->tm_vshare, v.v_pool, rows, rb, kAttnTileRows);
+        } else {
+            st = make_tmap(ctx, &cache->tm_kshare, v.k_pool, rows, c.head_dim, static_cast<uint32_t>(box));
+            if (st == KVZAP_OK) st = make_tmap(ctx, &cache->tm_vshare, v.v_pool, rows, c.head_dim, static_cast<uint32_t>(box));
+        }
         if (st != KVZAP_OK) return st;
-        KVZAP_CUDA(ctx, cudaFuncSetAttribute(shared_kernel(c.head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(sh_smem_bytes(c.head_dim))));
+        KVZAP_CUDA(ctx, cudaFuncSetAttribute(shared_kernel(d_attn, fp8), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(sh_smem_bytes(d_attn, fp8))));
         cache->share_box = box;
     }
     const int32_t *start = cache->share_meta + 1, *member = start + B + 1;
@@ -3494,20 +3505,25 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     return KVZAP_OK;
 }
 
-kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end, const void *Q,
-                                           int32_t n_q_heads, float scale, void *O, void *stream_)
+}  // extern "C"
+
+namespace kvzap {
+
+static kvzap_status attention_shared_impl(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end, const void *Q,
+                                          int32_t n_q_heads, float scale, void *O, void *stream_, bool fp8)
 {
-    NvtxRange nvtx_range("kvzap_decode_attention_shared");
+    NvtxRange nvtx_range(fp8 ? "kvzap_decode_attention_shared_fp8" : "kvzap_decode_attention_shared");
     if (!ctx || !cache || cache->ctx != ctx) return KVZAP_ERR_INVALID_ARG;
-    if (cache->share_subs == 0) return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, false);
+    if (cache->share_subs == 0) return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, fp8);
     begin_op(ctx);
     const kvzap_config &c = ctx->cfg;
     const SharingView &v = cache->v;
     DeviceGuard guard(c.device);
-    kvzap_status st = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, false);
+    kvzap_status st = attention_check(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, fp8);
     if (st != KVZAP_OK) return st;
     if (n_q_heads != cache->share_q_heads)
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "attention: the groups were told for %d query heads (kvzap_cache_share)", cache->share_q_heads);
+    const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     SharedAttnParams p;
     memset(&p, 0, sizeof p);
@@ -3527,7 +3543,7 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
     p.box_rows = cache->share_box;
     p.scale_log2e = scale * 1.4426950408889634f;
     p.status = ctx->status_dev;
-    const size_t layer_bytes = B * n_q_heads * c.head_dim * 2;
+    const size_t layer_bytes = B * n_q_heads * d_attn * 2;
     for (int32_t l0 = layer_begin; l0 < layer_end; l0 += cache->share_layers) {
         const int32_t l1 = std::min(layer_end, l0 + cache->share_layers);
         const uint8_t *q = static_cast<const uint8_t *>(Q) + static_cast<size_t>(l0 - layer_begin) * layer_bytes;
@@ -3537,20 +3553,36 @@ kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, i
         p.q = reinterpret_cast<const uint16_t *>(q);
         const size_t slots = static_cast<size_t>(ctx->sm_count) + static_cast<size_t>(l1 - l0) * cache->share_subs * c.n_kv_heads;
         p.v.part = static_cast<const float *>(cache->share_part);
-        p.v.part_ml = reinterpret_cast<const float2 *>(p.v.part + slots * cache->share_rows_max * c.head_dim);
+        p.v.part_ml = reinterpret_cast<const float2 *>(p.v.part + slots * cache->share_rows_max * d_attn);
         {
             ProfScope prof(ctx, KVZAP_KERNEL_ATTENTION, stream);
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attrs[2];
-            make_launch(&cfg, attrs, dim3(static_cast<unsigned>(p.v.n_ctas)), dim3(kShThreads), sh_smem_bytes(c.head_dim), stream,
+            make_launch(&cfg, attrs, dim3(static_cast<unsigned>(p.v.n_ctas)), dim3(static_cast<unsigned>(sh_threads(fp8))), sh_smem_bytes(d_attn, fp8), stream,
                         !ctx->profiling, 1);
-            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, shared_kernel(c.head_dim), cache->tm_kshare, cache->tm_vshare, p));
+            KVZAP_CUDA(ctx, cudaLaunchKernelEx(&cfg, shared_kernel(d_attn, fp8), cache->tm_kshare, cache->tm_vshare, p));
         }
         ctx->launches += 1;
-        st = attention_impl(ctx, cache, l0, l1, q, n_q_heads, scale, o, stream_, false, &p.v);
+        st = attention_impl(ctx, cache, l0, l1, q, n_q_heads, scale, o, stream_, fp8, &p.v);
         if (st != KVZAP_OK) return st;
     }
     return KVZAP_OK;
+}
+
+}  // namespace kvzap
+
+extern "C" {
+
+kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end, const void *Q,
+                                           int32_t n_q_heads, float scale, void *O, void *stream)
+{
+    return attention_shared_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream, false);
+}
+
+kvzap_status kvzap_decode_attention_shared_fp8(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end, const void *Q,
+                                               int32_t n_q_heads, float scale, void *O, void *stream)
+{
+    return attention_shared_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream, true);
 }
 
 kvzap_status kvzap_cache_lengths(kvzap_cache *cache, int32_t *lengths, void *stream_)

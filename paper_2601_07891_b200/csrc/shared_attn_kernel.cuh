@@ -24,7 +24,13 @@
 // P overwrites the first half of S; the matrix unit takes a thread's products in order, so the next S, issued behind P V,
 // cannot overtake it.  O is rescaled only when the running maximum has grown by more than 2^8 since the last time (P then
 // stays below 2^8, and its 8 bits are relative): after a few tiles hardly ever.
+//
+// 8-bit rows (D E4M3 codes, fp32 scale, 12 unused bytes): a tile comes in as it lies in memory, into a ring of its own, and four more warps widen it to the bf16
+// tile that the products take (exact: bf16 holds every E4M3 value), a row per thread.  The rows' scales stay in fp32 beside the products: a column of S is multiplied
+// by its K row's scale ahead of the softmax, a column of P by its V row's behind it.
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include "decode_kernels.cuh"
 #include "ptx.cuh"
@@ -34,7 +40,7 @@ namespace kvzap {
 constexpr int kShMostCtas = 148;             // CTAs of a launch, and pieces of a list, at most
 constexpr int kShTile = 128;                 // shared rows per tile, rows of Q per group of warps
 constexpr int kShProducers = 3;              // warps that issue copies
-constexpr int kShThreads = 384;              // 2 x 4 softmax warps, producers, products
+__host__ __device__ constexpr int sh_threads(bool fp8) { return fp8 ? 512 : 384; }      // 2 x 4 softmax warps, producers, products; widening
 constexpr float kShGrow = 8.0f;              // powers of two by which the maximum may grow before O is rescaled
 
 // What decode_attn_kernel needs to find the slots of a list.
@@ -90,11 +96,16 @@ __device__ __forceinline__ int share_owner(int64_t tiles, int ctas, int64_t t)
     return i;
 }
 
-__host__ __device__ constexpr int sh_stages(int d) { return d == 128 ? 5 : 9; }
+__host__ __device__ constexpr int sh_stages(int d, bool fp8) { return fp8 ? (d == 128 ? 3 : 5) : d == 128 ? 5 : 9; }
 __host__ __device__ constexpr uint32_t sh_stage_bytes(int d) { return kShTile * d * 2u; }
-__host__ __device__ constexpr uint32_t sh_smem_bytes(int d)
+// 8-bit rows: tiles as they lie in memory, and the scales of the last kShScales tiles.  A tile's scales are read until P of it is there, and a buffer is free
+// for the K tile four further on only when the products of that P are done (3 or 5 buffers, two a tile).
+constexpr int kShScales = 4;
+__host__ __device__ constexpr uint32_t sh_raw_bytes(int d) { return kShTile * (d + 16u); }
+__host__ __device__ constexpr uint32_t sh_smem_bytes(int d, bool fp8)
 {
-    return 1024u + sh_stages(d) * sh_stage_bytes(d) + 2u * sh_stage_bytes(d) /* Q */ + 512u /* barriers */;
+    return 1024u + (sh_stages(d, fp8) + 2u /* Q */) * sh_stage_bytes(d) + 512u /* barriers */ +
+           (fp8 ? sh_stages(d, fp8) * sh_raw_bytes(d) + kShScales * 2u * kShTile * 4u : 0u);
 }
 
 __device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t *r)
@@ -287,7 +298,7 @@ struct SharePiece {
     int32_t leader;                 // list of a member that does
 };
 struct ShareRun { int64_t at, end, base; int unit; };      // tiles of the call [at, end), the first of list `unit`; tiles ahead of the call
-// Whole CTA; one round trip to memory for up to kShThreads lists.
+// Whole CTA; one round trip to memory for as many lists as it has threads.
 __device__ __forceinline__ ShareRun share_my_run(const SharedAttnParams &p)
 {
     __shared__ int unit_s;
@@ -301,7 +312,7 @@ __device__ __forceinline__ ShareRun share_my_run(const SharedAttnParams &p)
         r.at = share_run(tiles, ctas, blockIdx.x);
         r.end = share_run(tiles, ctas, blockIdx.x + 1);
     }
-    for (int u = threadIdx.x; u < n_units; u += kShThreads) {
+    for (int u = threadIdx.x; u < n_units; u += blockDim.x) {
         const int64_t first = __ldg(&lists[u].x) - r.base, last = __ldg(&lists[u + 1].x) - r.base;
         if (first <= r.at && r.at < last) unit_s = u;
     }
@@ -331,9 +342,12 @@ __device__ __forceinline__ bool share_next(const SharedAttnParams &p, ShareRun &
     return false;
 }
 
-// Registers of the calling warpgroup from here on.  The block is launched with 384 x 168; 256 x 216 + 128 x 72 is the same.
-constexpr int kShRegsSoftmax = 216, kShRegsOthers = 72;
-static_assert(256 * kShRegsSoftmax + 128 * kShRegsOthers <= kShThreads * 168, "no more than the block has");
+// Registers of the calling warpgroup from here on.  The block is launched with 384 x 168; 256 x 216 + 128 x 72 is the same.  8-bit rows: 512 x 128, 256 x 168 + 128 x 80 + 128 x 96.
+__host__ __device__ constexpr int sh_regs_softmax(bool fp8) { return fp8 ? 168 : 216; }
+__host__ __device__ constexpr int sh_regs_others(bool fp8) { return fp8 ? 80 : 72; }
+constexpr int kShRegsWiden = 96;
+static_assert(256 * sh_regs_softmax(false) + 128 * sh_regs_others(false) <= 384 * 168, "no more than the block has");
+static_assert(256 * sh_regs_softmax(true) + 128 * sh_regs_others(true) + 128 * kShRegsWiden <= 512 * 128, "no more than the block has");
 __device__ __forceinline__ void named_barrier_arrive(uint32_t id, uint32_t n_threads)
 {
     asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n_threads) : "memory");
@@ -351,12 +365,31 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v)
 __device__ __forceinline__ int sh_k_pos(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int sh_v_pos(int t, int n) { return t + 1 < n ? 2 * t + 2 : 2 * n - 1; }
 
-template <int kD>
-__global__ void __launch_bounds__(kShThreads, 1)
+// sixteen E4M3 codes -> bf16, in order
+__device__ __forceinline__ void e4m3x16_to_bf16(const uint4 &codes, uint4 &lo, uint4 &hi)
+{
+    const uint32_t in[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint32_t out[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t h[2];
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(h[0]), "=r"(h[1]) : "r"(in[i]));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
+            out[2 * i + j] = pack_bf16x2(f.x, f.y);
+        }
+    }
+    lo = make_uint4(out[0], out[1], out[2], out[3]);
+    hi = make_uint4(out[4], out[5], out[6], out[7]);
+}
+
+template <int kD, bool kFp8>
+__global__ void __launch_bounds__(sh_threads(kFp8), 1)
 shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const SharedAttnParams p)
 {
-    constexpr int kHalves = kD / 64;
-    constexpr int kStages = sh_stages(kD);
+    constexpr int kHalves = kFp8 ? 1 : kD / 64;                             // copies side by side for the same rows
+    constexpr int kStages = sh_stages(kD, kFp8);
     constexpr uint32_t kStageBytes = sh_stage_bytes(kD);
     constexpr uint32_t kHalfBytes = kShTile * 128u;
     extern __shared__ uint8_t sh_smem_raw[];
@@ -368,12 +401,22 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t bars = qtile + 2 * kStageBytes;
     const uint32_t full = bars, empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16,
                    q_full = p_full + 32, done = q_full + 8, o_free = done + 8;
+    // 8-bit rows: [kStages] tiles as they lie in memory with barriers of their own, [kShScales][K, V][kShTile] scales, told by tile and kind
+    const uint32_t raw_full = o_free + 8, raw_empty = raw_full + 8 * kStages, scales_full = raw_empty + 8 * kStages;
+    static_assert(8 * (2 * kStages + 2 + 4 + 3) + (kFp8 ? 8 * (2 * kStages + 2 * kShScales) : 0) <= 512, "room for the barriers");
+    constexpr uint32_t kRawBytes = sh_raw_bytes(kD), kRowBytes8 = kD + 16;
+    const uint32_t raw = bars + 512;
+    float *scales = reinterpret_cast<float *>(smem + (kStages + 2) * kStageBytes + 512 + kStages * kRawBytes);
     __shared__ uint32_t tmem_s;
     __shared__ volatile int abort_s, failed_s;         // a wait ran out; in a softmax warp
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kShProducers); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kFp8 ? 128 : kShProducers); mbar_init(empty + 8 * i, 1); }
+        if (kFp8) {
+            for (int i = 0; i < kStages; ++i) { mbar_init(raw_full + 8 * i, kShProducers); mbar_init(raw_empty + 8 * i, 128); }
+            for (int i = 0; i < 2 * kShScales; ++i) mbar_init(scales_full + 8 * i, 128);
+        }
         for (int w = 0; w < 2; ++w) { mbar_init(s_full + 8 * w, 1); mbar_init(p_full + 16 * w, 128); mbar_init(p_full + 16 * w + 8, 128); }
         mbar_init(q_full, 256);
         mbar_init(done, 1);
@@ -401,15 +444,51 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     bool ok = true;
     const CacheView &c = p.c;
 
-    if (warp >= 8) {
-        regs_fewer<kShRegsOthers>();          // the whole warpgroup, at this one place
+    if (kFp8 && warp >= 12) {
+        // ---- widening: thread = row of the tile
+        regs_fewer<kShRegsWiden>();
+        const int r = threadIdx.x - 384;
+        while (ok && share_next(p, walk, x)) {
+            const int n = x.t1 - x.t0;
+            auto widen = [&](uint32_t pos, int t, int kind) {
+                const uint32_t i = pos0 + pos, stage = i % kStages, round = i / kStages, tile = pos0 / 2 + t;
+                ok = __all_sync(0xffffffffu, mbar_wait(raw_full + 8 * stage, round & 1, &abort_s) &&
+                                             (round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s)));
+                if (!ok) return;
+                if (r < x.n_rows - (x.t0 + t) * kShTile) {                    // what lies behind the list's end is not looked at
+                    const uint8_t *src = smem + (raw - ring) + stage * kRawBytes + r * kRowBytes8;
+                    uint8_t *dst = smem + stage * kStageBytes + r * 128;
+#pragma unroll
+                    for (int u = 0; u < kD / 8; u += 2) {
+                        uint4 lo, hi;
+                        e4m3x16_to_bf16(*reinterpret_cast<const uint4 *>(src + u * 8), lo, hi);
+                        *reinterpret_cast<uint4 *>(dst + (u >> 3) * kHalfBytes + (((u & 7) ^ (r & 7)) << 4)) = lo;
+                        *reinterpret_cast<uint4 *>(dst + (u >> 3) * kHalfBytes + ((((u & 7) + 1) ^ (r & 7)) << 4)) = hi;
+                    }
+                    scales[((tile % kShScales) * 2 + kind) * kShTile + r] = *reinterpret_cast<const float *>(src + kD);
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(scales_full + 8 * ((tile % kShScales) * 2 + kind));
+                mbar_arrive(full + 8 * stage);
+                mbar_arrive(raw_empty + 8 * stage);
+            };
+            widen(0, 0, 0);
+            for (int t = 0; ok && t < n; ++t) {
+                if (t + 1 < n) widen(sh_k_pos(t + 1), t + 1, 0);
+                if (ok) widen(sh_v_pos(t, n), t, 1);
+            }
+            pos0 += 2 * n;
+        }
+    } else if (warp >= 8) {
+        regs_fewer<sh_regs_others(kFp8)>();   // the whole warpgroup, at this one place
         if (warp < 8 + kShProducers) {
             named_barrier_sync(4, 256 + 32 * kShProducers);       // the queries' loads are on their way: behind a ring full of rows they took 6 us
             // ---- copies.  A tile is n_boxes x kHalves boxes, numbered with the halves fastest; lane i of producer q has number q + kShProducers i
             const int n_boxes = kShTile / p.box_rows, mine = warp - 8 + kShProducers * lane;
             const int box = mine / kHalves, half = mine % kHalves;
             const uint64_t policy = l2_policy_evict_first();
-            const uint32_t box_bytes = p.box_rows * 128u;
+            const uint32_t box_bytes = p.box_rows * (kFp8 ? kRowBytes8 : 128u);
+            const uint32_t to_full = kFp8 ? raw_full : full, to_empty = kFp8 ? raw_empty : empty;
             while (ok && share_next(p, walk, x)) {
                 const int n = x.t1 - x.t0;
                 const int32_t *pages = c.page_table + static_cast<int64_t>(x.leader) * c.max_pages;
@@ -424,11 +503,14 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 };
                 auto copy = [&](const CUtensorMap *map, uint32_t pos, const Place &at) {
                     const uint32_t i = pos0 + pos, stage = i % kStages, round = i / kStages;
-                    if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
+                    if (!__all_sync(0xffffffffu, round == 0 || mbar_wait(to_empty + 8 * stage, (round - 1) & 1, &abort_s))) { ok = false; return; }
                     const uint32_t who = __ballot_sync(0xffffffffu, at.row >= 0);
-                    if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, __popc(who) * box_bytes);
+                    if (lane == 0) mbar_arrive_expect_tx(to_full + 8 * stage, __popc(who) * box_bytes);
                     __syncwarp();
-                    if (at.row >= 0)
+                    if (at.row < 0) return;
+                    if constexpr (kFp8)
+                        tma_load_3d(raw + stage * kRawBytes + box * box_bytes, map, to_full + 8 * stage, 0, 0, (at.page * c.page_tokens + at.row) / 16, policy);
+                    else
                         tma_load_2d(ring + stage * kStageBytes + half * kHalfBytes + box * box_bytes, map, full + 8 * stage, half * 64,
                                     at.page * c.page_tokens + at.row, policy);
                 };
@@ -516,11 +598,11 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
     } else {
         // ---- softmax: thread = row of Q
-        regs_more<kShRegsSoftmax>();
+        regs_more<sh_regs_softmax(kFp8)>();
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + lanes + 256 * w, to = ts + 128;
-        uint32_t n_s = 0, n_piece = 0;
+        uint32_t n_s = 0, n_piece = 0, tiles_before = 0;
         // The piece's rows of Q: of one tile 16 a warp, of two 32; a lane finds the place of one of them (in units of 16 bytes), then 32 lanes load whole
         // rows.  Rows past the members' read the last one's, and are zeros.  Sent for while the piece before is brought to its end (there are no
         // registers to load them to).  Short code: in a launch's first microseconds instructions are waited for like data.
@@ -545,6 +627,16 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const uint4 *from = reinterpret_cast<const uint4 *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(at_q), r & 31));
                 q[k] = __ldg(from + lane % kUnits);                  // of one tile the second half is not used
                 if (row0 + r >= n_rows_q) q[k] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        };
+        auto scale_columns = [&](uint32_t *v, const float *by) {     // 64 of them
+#pragma unroll
+            for (int k = 0; k < 64; k += 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(by + k);
+                v[k] = __float_as_uint(__uint_as_float(v[k]) * f.x);
+                v[k + 1] = __float_as_uint(__uint_as_float(v[k + 1]) * f.y);
+                v[k + 2] = __float_as_uint(__uint_as_float(v[k + 2]) * f.z);
+                v[k + 3] = __float_as_uint(__uint_as_float(v[k + 3]) * f.w);
             }
         };
         bool have = share_next(p, walk, x);
@@ -580,6 +672,12 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 n_s += 1;
                 tc_fence_after_sync();
                 const int rows = x.n_rows - (x.t0 + t) * kShTile;
+                const uint32_t tile = tiles_before + t;
+                const float *k_scales = scales + (tile % kShScales) * 2 * kShTile, *v_scales = k_scales + kShTile;
+                if constexpr (kFp8) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(scales_full + 16 * (tile % kShScales), (tile / kShScales) & 1, &abort_s) &&
+                                                 mbar_wait(scales_full + 16 * (tile % kShScales) + 8, (tile / kShScales) & 1, &abort_s))) { ok = false; break; }
+                }
                 // the row in pieces of 32 columns, from tensor memory twice: rolled, the code of a step is there after a few misses of the instruction cache
                 float mx = -INFINITY;
 #pragma unroll 1
@@ -590,6 +688,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     tmem_wait_ld();
                     reg_fence32(s);
                     reg_fence32(s + 32);
+                    if constexpr (kFp8) scale_columns(s, k_scales + 32 * j);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         float m16 = fmaxf(__uint_as_float(s[16 * g]), __uint_as_float(s[16 * g + 1]));
@@ -630,6 +729,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     tmem_wait_ld();
                     reg_fence32(s);
                     reg_fence32(s + 32);
+                    if constexpr (kFp8) scale_columns(s, k_scales + 32 * j);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {                // 16 columns at a time
                         uint32_t pk[8];
@@ -643,6 +743,10 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             a = fast_ex2(a); b = fast_ex2(b); d = fast_ex2(d); e = fast_ex2(e);
                             sum2 = k == 0 ? f2_pack(a, b) : f2_add(sum2, f2_pack(a, b));
                             sum2b = k == 0 ? f2_pack(d, e) : f2_add(sum2b, f2_pack(d, e));
+                            if constexpr (kFp8) {
+                                const float4 vs = *reinterpret_cast<const float4 *>(v_scales + 32 * j + 16 * g + k);
+                                a *= vs.x; b *= vs.y; d *= vs.z; e *= vs.w;
+                            }
                             pk[k / 2] = pack_bf16x2(a, b);       // P: 8 bits, relative to the row's maximum; the sum takes all 24
                             pk[k / 2 + 1] = pack_bf16x2(d, e);
                         }
@@ -677,6 +781,7 @@ shared_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             tc_fence_after_sync();
             if (failed_s) ok = false;
             n_piece += 1;
+            tiles_before += n;
             x = after;
             if (!ok) {                                            // a wait ran out: the outputs that this piece is part of are zeros
                 for (int r = threadIdx.x; r < n_rows_q; r += 256) ml_out[r] = make_float2(-INFINITY, -1.0f);

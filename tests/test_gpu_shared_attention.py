@@ -412,7 +412,7 @@ def test_refusals(binding):
     refused(lambda: s.cache.attention_shared(0, 1, Q, scale=float("nan")), 1, "scale")
     assert lib.kvzap_decode_attention_shared(s.ctx.handle, s.cache.handle, 0, 1, None, 8, 1.0, Q.data_ptr(), None) == 1
     s.check(8)
-    for kw in (dict(D=72, w=16, page=16), dict(D=128, w=8, page=16), dict(D=128, w=16, page=24)):
+    for kw in (dict(D=80, w=16, page=16), dict(D=128, w=8, page=16), dict(D=128, w=16, page=24)):
         other = Setup(binding, 2, 1, 2, kw["D"], kw["w"], kw["page"], 20)
         refused(lambda: other.cache.share([[0, 1]], 8), 2, "multiples")
 
@@ -498,3 +498,108 @@ def test_many_long_own_lists(binding):
     s.cache.fork([0, 0], [38, 39])
     s.cache.share([[0, 38, 39], list(range(1, 38))], H)
     s.check(H)
+
+
+class Setup8(Setup):
+    """The same over 8-bit rows of D codes: rows of all sizes of scale, pools that hold NaN codes and scales elsewhere."""
+
+    def __init__(self, binding, B, L, H, D, w, page, width, **kw):
+        super().__init__(binding, B, L, H, (D + 16) // 2, w, page, width, **kw)
+        self.codes = D
+
+    def normal(self, *shape):
+        from paper_2601_07891_b200 import synth
+        if shape[-1] != self.D:
+            return super().normal(*shape)
+        x = torch.empty(*shape[:-1], self.codes, device="cuda").normal_(generator=self.g)
+        x *= torch.empty(*shape[:-1], 1, device="cuda").uniform_(0.25, 4.0, generator=self.g)
+        return synth.pack_rows_e4m3(x.view(-1, self.codes)).view(*shape[:-1], self.D)
+
+    def rows8(self, packed):
+        b = packed.view(torch.uint8)
+        return b[:, :self.codes].contiguous().view(torch.float8_e4m3fn).double() * b[:, self.codes:self.codes + 4].contiguous().view(torch.float32).double()
+
+    def check8(self, n_q_heads, layers=None, spread=1.0):
+        layers = list(range(self.L)) if layers is None else layers
+        G = n_q_heads // self.H
+        Q = torch.empty(len(layers), self.B, n_q_heads, self.codes, dtype=torch.bfloat16, device="cuda").normal_(generator=self.g) * spread
+        O, scale = torch.full_like(Q, 7.0), self.codes ** -0.5
+        self.binding.kvzap_decode_attention_shared_fp8(self.ctx.handle, self.cache.handle, layers[0], layers[-1] + 1, Q, scale, O)
+        torch.cuda.synchronize()
+        assert self.ctx.poll_status() == 0
+        K, V, start, _, _ = self.cache.pack(list(range(self.B)))
+        K, V, start = self.rows8(K), self.rows8(V), start.tolist()
+        assert bool(torch.isfinite(O).all())
+        for i, l in enumerate(layers):
+            for b in range(self.B):
+                for h in range(self.H):
+                    j = (b * self.L + l) * self.H + h
+                    got = O[i, b, h * G:(h + 1) * G].double()
+                    if start[j] == start[j + 1]:
+                        assert bool((got == 0).all())
+                        continue
+                    k, v = K[start[j]:start[j + 1]], V[start[j]:start[j + 1]]
+                    p = torch.softmax(Q[i, b, h * G:(h + 1) * G].double() @ k.t() * scale, -1)
+                    want, A = p @ v, p @ v.abs()
+                    assert bool(((got - want).abs() <= want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10)).all()), (l, b, h)
+        return O
+
+
+@pytest.mark.parametrize("members,G,D,page,w,low,high,steps", [
+    (2, 4, 128, 16, 16, 128, 400, 3),
+    (2, 1, 64, 16, 0, 100, 700, 0),
+    (5, 7, 64, 80, 16, 300, 900, 20),
+    (17, 8, 128, 48, 32, 500, 1100, 40),    # two tiles of query rows
+    (33, 8, 128, 16, 16, 300, 2600, 5),     # the group in two parts
+    (70, 4, 64, 256, 16, 256, 1200, 5),
+])
+def test_rows_of_8_bits(binding, members, G, D, page, w, low, high, steps):
+    H = 3
+    width = high // page + (steps + w) // page + 3
+    s = Setup8(binding, members, 2, H, D, w, page, width, n_pages=2 * H * (width + members * (steps // page + 3)), seed=members)
+    s.fill(0, _ragged(2 * H, low, high, members), tokens=5 if w else 0)
+    s.cache.fork([0] * (members - 1), list(range(1, members)))
+    s.steps(steps)
+    s.cache.share([list(range(members))], H * G)
+    first = s.check8(H * G)
+    assert first.shape[-1] == D
+    s.check8(H * G, layers=[1], spread=3.0)
+    s.cache.release_seq(0)
+    s.check8(H * G)
+
+
+def test_rows_of_8_bits_long_and_in_groups(binding):
+    s = Setup8(binding, 9, 1, 2, 128, 16, 16, 1300, n_pages=8000, seed=21)
+    s.fill(0, [20000, 3111])
+    s.fill(5, [130, 700])
+    s.cache.fork([0] * 4, [1, 2, 3, 4])
+    s.cache.fork([5, 5], [6, 7])
+    s.steps(30)
+    s.cache.share([[4, 0, 2, 1, 3], [7, 5, 6, 8]], 8)
+    a = s.check8(8)
+    Q = torch.empty_like(a).normal_()
+    outs = []
+    for _ in range(10):
+        O = torch.empty_like(Q)
+        binding.kvzap_decode_attention_shared_fp8(s.ctx.handle, s.cache.handle, 0, 1, Q, 0.1, O)
+        outs.append(O)
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+def test_8_bit_and_bf16_calls_keep_to_their_rows(binding):
+    s8 = Setup8(binding, 2, 1, 2, 128, 16, 16, 30, seed=22)
+    s = Setup(binding, 2, 1, 2, 128, 16, 16, 30, seed=22)
+    for x in (s8, s):
+        x.fill(0, 200)
+        x.cache.fork([0], [1])
+        x.cache.share([[0, 1]], 8)
+    Q = torch.zeros(1, 2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    O = torch.empty_like(Q)
+    with pytest.raises(binding.KvzapError) as e:
+        binding.kvzap_decode_attention_shared(s8.ctx.handle, s8.cache.handle, 0, 1, Q, 1.0, O)
+    assert e.value.status == 2
+    with pytest.raises(binding.KvzapError) as e:
+        binding.kvzap_decode_attention_shared_fp8(s.ctx.handle, s.cache.handle, 0, 1, Q, 1.0, O)
+    assert e.value.status == 2
+    s8.check8(8)
+    s.check(8)
