@@ -570,17 +570,20 @@ kvzap_status kvzap_cache_unpack(kvzap_cache *cache, const int32_t *seqs, int32_t
  * released, forked into, unpacked into or imported over counts as alone from then on, the others go on sharing.
  *   group_start [n_groups + 1], seqs int32, HOST (read before return); a slot is in one group at most, others are read by themselves
  *   n_q_heads: query heads of the attention calls to come (1..8 times the KV heads)
- * n_groups = 0 takes all groups back.  The first call allocates device memory (up to some 64 MB, or what one layer needs; more only
- * for larger groups), a later one may.  Same limits on D, pages and window as kvzap_decode_attention and kvzap_decode_attention_fp8.
+ *   flags: 0, or KVZAP_SHARE_ALWAYS.  Reading together takes a second launch and some 8 us; a call over layers in which it saves
+ *     less than 160 MB of rows (300 MB of 8-bit rows) takes about as long or longer and reads every list by itself, unless the flag is set
+ * n_groups = 0 takes all groups back.  Synchronises `stream` (the host is told what is saved).  The first call allocates device
+ * memory (up to some 64 MB, or what one layer needs; more only for larger groups), a later one may.  Same limits on D, pages and window as kvzap_decode_attention and kvzap_decode_attention_fp8.
  */
+#define KVZAP_SHARE_ALWAYS 1
 kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, const int32_t *seqs, int32_t n_groups,
-                               int32_t n_q_heads, void *stream);
+                               int32_t n_q_heads, int32_t flags, void *stream);
 
 /*
  * kvzap_decode_attention over a cache with groups (kvzap_cache_share): the same operation with the same arguments, but the rows
  * that a group shares are read once for all its members.  Results differ from kvzap_decode_attention's by rounding only,
- * whatever was released or forked since the groups were told.  Without groups it is that call.  Two launches (for many layers
- * some pairs of them).  KVZAP_ERR_INVALID_ARG for another n_q_heads than the groups were told for.
+ * whatever was released or forked since the groups were told.  Without groups, or with little to save, it is that call.  Two
+ * launches (for many layers some pairs of them).  KVZAP_ERR_INVALID_ARG for another n_q_heads than the groups were told for.
  * In a captured graph the groups are those of the capture; a replay after another kvzap_cache_share reads every list by itself.
  */
 kvzap_status kvzap_decode_attention_shared(kvzap_ctx *ctx, kvzap_cache *cache, int32_t layer_begin, int32_t layer_end,

@@ -97,7 +97,7 @@ SIGNATURES = {
     "kvzap_cache_fork": (_i32, [_vp, _vp, _vp, _i32, _vp]),
     "kvzap_cache_pack": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp]),
     "kvzap_cache_unpack": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp]),
-    "kvzap_cache_share": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp]),
+    "kvzap_cache_share": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _vp]),
     "kvzap_decode_attention_shared": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_decode_attention_shared_fp8": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_set_rotary": (_i32, [_vp, ctypes.POINTER(KvzapRotaryConfig)]),
@@ -420,13 +420,16 @@ def kvzap_cache_unpack(handle, cache, seqs, K, V, row_start, n_tokens, scores, s
                                              _ptr(n_tokens), _ptr(scores), _stream(stream)))
 
 
-def kvzap_cache_share(handle, cache, groups, n_q_heads, stream=None):
+SHARE_ALWAYS = 1
+
+
+def kvzap_cache_share(handle, cache, groups, n_q_heads, flags=0, stream=None):
     """groups: lists of slot numbers (host)."""
     start = [0]
     for g in groups:
         start.append(start[-1] + len(g))
     _check(handle, load().kvzap_cache_share(cache, _ints(start), _ints([b for g in groups for b in g]), len(groups), n_q_heads,
-                                            _stream(stream)))
+                                            flags, _stream(stream)))
 
 
 def kvzap_decode_attention_shared(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None):
@@ -862,9 +865,10 @@ class KvzapCache:
         kvzap_decode_attention(self.ctx.handle, self.handle, layer_begin, layer_end, Q, scale, out, stream)
         return out
 
-    def share(self, groups, n_q_heads, stream=None):
-        """Lists of slots whose common leading pages attention_shared() reads once for all of them; [] takes all groups back."""
-        kvzap_cache_share(self.ctx.handle, self.handle, groups, n_q_heads, stream)
+    def share(self, groups, n_q_heads, always=False, stream=None):
+        """Lists of slots whose common leading pages attention_shared() reads once for all of them; [] takes all groups back.  Calls that
+        would save little read every list by itself, unless `always`."""
+        kvzap_cache_share(self.ctx.handle, self.handle, groups, n_q_heads, SHARE_ALWAYS if always else 0, stream)
 
     def attention_shared(self, layer_begin, layer_end, Q, scale=None, out=None, stream=None):
         """attention() with the rows that the groups told by share() have in common read once for each group."""

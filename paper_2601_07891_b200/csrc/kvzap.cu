@@ -2545,6 +2545,8 @@ struct kvzap_cache {
     void *share_part = nullptr;          // slots of (m, l), then of outputs
     size_t share_part_bytes = 0;
     int32_t share_layers = 0;            // layers of a launch, as far as the slots go
+    std::vector<int64_t> share_saved;    // [L + 1] rows that members would read again, of the layers ahead
+    bool share_always = false;
 };
 
 namespace kvzap {
@@ -3388,7 +3390,7 @@ kvzap_status kvzap_cache_unpack(kvzap_cache *cache, const int32_t *seqs, int32_t
 }
 
 kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, const int32_t *seqs, int32_t n_groups, int32_t n_q_heads,
-                               void *stream_)
+                               int32_t flags, void *stream_)
 {
     NvtxRange nvtx_range("kvzap_cache_share");
     if (!cache) return KVZAP_ERR_INVALID_ARG;
@@ -3396,6 +3398,7 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     begin_op(ctx);
     const kvzap_config &c = ctx->cfg;
     const SharingView &v = cache->v;
+    if ((flags & ~KVZAP_SHARE_ALWAYS) != 0) return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: unknown flags %d", flags);
     if (n_groups < 0 || (n_groups > 0 && (!group_start || !seqs)))
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "share: group_start and seqs (host), n_groups >= 0 are required");
     if (n_q_heads < c.n_kv_heads || n_q_heads % c.n_kv_heads != 0 || n_q_heads / c.n_kv_heads > kAttnMaxGroup)
@@ -3498,6 +3501,19 @@ kvzap_status kvzap_cache_share(kvzap_cache *cache, const int32_t *group_start, c
     share_scan_kernel<<<1, 1024, 0, stream>>>(cache->share_lists, static_cast<int>(units));
     KVZAP_CUDA(ctx, cudaGetLastError());
     ctx->launches += 2;
+    // Rows that need not be read again, ahead of each layer; lists are in the order of layers.
+    try {
+        std::vector<int4> lists(units);
+        KVZAP_CUDA(ctx, cudaMemcpyAsync(lists.data(), cache->share_lists, sizeof(int4) * units, cudaMemcpyDeviceToHost, stream));
+        KVZAP_CUDA(ctx, cudaStreamSynchronize(stream));
+        cache->share_saved.assign(static_cast<size_t>(c.n_layers) + 1, 0);
+        for (unsigned u = 0; u < units; ++u)
+            cache->share_saved[u / per_layer + 1] += static_cast<int64_t>(lists[u].y) * std::max((lists[u].w & 511) - 1, 0);
+        for (int l = 0; l < c.n_layers; ++l) cache->share_saved[l + 1] += cache->share_saved[l];
+    } catch (...) {
+        return fail(ctx, KVZAP_ERR_CUDA, "out of host memory");
+    }
+    cache->share_always = (flags & KVZAP_SHARE_ALWAYS) != 0;
     cache->share_subs = n_subs;
     cache->share_q_heads = n_q_heads;
     cache->share_rows_max = rows_max;
@@ -3515,7 +3531,6 @@ static kvzap_status attention_shared_impl(kvzap_ctx *ctx, kvzap_cache *cache, in
     NvtxRange nvtx_range(fp8 ? "kvzap_decode_attention_shared_fp8" : "kvzap_decode_attention_shared");
     if (!ctx || !cache || cache->ctx != ctx) return KVZAP_ERR_INVALID_ARG;
     if (cache->share_subs == 0) return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, fp8);
-    begin_op(ctx);
     const kvzap_config &c = ctx->cfg;
     const SharingView &v = cache->v;
     DeviceGuard guard(c.device);
@@ -3523,6 +3538,15 @@ static kvzap_status attention_shared_impl(kvzap_ctx *ctx, kvzap_cache *cache, in
     if (st != KVZAP_OK) return st;
     if (n_q_heads != cache->share_q_heads)
         return fail(ctx, KVZAP_ERR_INVALID_ARG, "attention: the groups were told for %d query heads (kvzap_cache_share)", cache->share_q_heads);
+    // Whether reading together pays goes by the bytes that it saves: about 160 MB of rows take as long as the second launch and the
+    // joins.  Measured with 8 heads, saved MB: us read together / by themselves.  1 layer x 4 members 49: 25 / 15, 197: 38 / 29; 1 x 8
+    // 115: 23 / 19, 229: 28 / 29; 1 x 32 38: 20 / 15, 127: 22 / 22, 254: 24 / 33; 4 x 4 98: 24 / 20, 197: 28 / 30; 4 x 16 74: 24 / 19,
+    // 246: 26 / 40.  8-bit rows, which are widened on the way: 1 x 8 129: 36 / 31, 258: 45 / 50; 1 x 32 71: 27 / 24, 143: 29 / 36; 4 x 4
+    // 221: 55 / 46; 4 x 16 138: 33 / 40; 1 x 16 with 8 query heads to each 277: 55 / 53, 553: 63 / 93.
+    const int64_t saved = (cache->share_saved[layer_end] - cache->share_saved[layer_begin]) * c.head_dim * 4;
+    if (!cache->share_always && saved < (fp8 ? 300000000 : 160000000))
+        return attention_impl(ctx, cache, layer_begin, layer_end, Q, n_q_heads, scale, O, stream_, fp8);
+    begin_op(ctx);
     const int d_attn = fp8 ? c.head_dim * 2 - kAttnTrailerBytes : c.head_dim;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     SharedAttnParams p;

@@ -6,6 +6,7 @@ here), exponentials are within 2^-20 of themselves, logits within 128 2^-24 of t
 here, sizes below 2^4: 2^-8 ... of a tenth of the weight at most), and the output is rounded once, half a step, 2^-8 of itself.  Altogether
 2^-8 |O| + (2^-8 + 2^-10) sum p |v|.
 """
+import functools
 import random
 
 import pytest
@@ -36,6 +37,7 @@ class Setup:
         self.K_pool = torch.full((n_pages, page, D), float("nan"), dtype=torch.bfloat16, device="cuda")
         self.V_pool = torch.full_like(self.K_pool, float("nan"))
         self.cache = self.ctx.create_cache(B, w, page, self.K_pool, self.V_pool, width)
+        self.cache.share = functools.partial(self.cache.share, always=True)       # whatever it saves
         for b in range(B):
             self.cache.release_seq(b)
 
@@ -401,9 +403,10 @@ def test_refusals(binding):
     lib = binding.load()
     ints = binding._ints
     for start in ([1, 2], [0, -1], [0, 5], [0, 2, 1]):
-        assert lib.kvzap_cache_share(s.cache.handle, ints(start), ints([0, 1, 2, 3]), len(start) - 1, 8, None) == 1
-    assert lib.kvzap_cache_share(s.cache.handle, None, None, 1, 8, None) == 1
-    assert lib.kvzap_cache_share(s.cache.handle, None, None, -1, 8, None) == 1
+        assert lib.kvzap_cache_share(s.cache.handle, ints(start), ints([0, 1, 2, 3]), len(start) - 1, 8, 0, None) == 1
+    assert lib.kvzap_cache_share(s.cache.handle, None, None, 1, 8, 0, None) == 1
+    assert lib.kvzap_cache_share(s.cache.handle, None, None, -1, 8, 0, None) == 1
+    assert lib.kvzap_cache_share(s.cache.handle, ints([0, 2]), ints([0, 1]), 1, 8, 2, None) == 1
     s.cache.share([[0, 1]], 8)
     Q = s.normal(1, 4, 8, 128)
     refused(lambda: s.cache.attention_shared(0, 1, s.normal(1, 4, 4, 128)), 1, "told for 8")
@@ -446,7 +449,7 @@ def test_forks_between_steps_that_overlap(binding, hidden, grouped):
                    lambda: cache.fork([2, 2, 2], [0, 1, 4])):
         change()
         if grouped:
-            cache.share([[0, 1, 2], [3, 4]], H * G)
+            cache.share([[0, 1, 2], [3, 4]], H * G, always=True)
         for _ in range(6):
             X, K, V, Q = normal(L, B, 256), normal(L, B, H, D), normal(L, B, H, D), normal(L, B, H * G, D)
             O = torch.empty_like(Q)
@@ -603,3 +606,25 @@ def test_8_bit_and_bf16_calls_keep_to_their_rows(binding):
     assert e.value.status == 2
     s8.check8(8)
     s.check(8)
+
+
+def test_little_to_save_is_read_by_itself(binding):
+    """The rule goes by the rows that the call's layers save; either way the results are right."""
+    s = Setup(binding, 12, 3, 8, 128, 16, 16, 700, n_pages=3 * 8 * 900, seed=23)
+    s.fill(0, [200] * 8 + [10000] * 8 + [900] * 8)
+    s.cache.fork([0] * 11, list(range(1, 12)))
+    s.steps(2)
+
+    def launches(layers):
+        Q = s.normal(len(layers), 12, 32, 128)
+        before = s.ctx.launch_count()
+        O = s.cache.attention_shared(layers[0], layers[-1] + 1, Q)
+        n = s.ctx.launch_count() - before
+        want, A = s.want(Q, 128 ** -0.5, layers)
+        assert bool(((O.double() - want).abs() <= want.abs() * 2.0 ** -8 + A * (2.0 ** -8 + 2.0 ** -10)).all())
+        return n
+
+    s.cache.share([list(range(12))], 32, always=False)
+    assert [launches([0]), launches([1]), launches([2]), launches([0, 1, 2])] == [1, 2, 1, 2]
+    s.cache.share([list(range(12))], 32)
+    assert [launches([0]), launches([1]), launches([2])] == [2, 2, 2]

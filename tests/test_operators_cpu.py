@@ -9,7 +9,7 @@ def test_calls_without_a_handle_are_refused():
     assert lib.kvzap_cache_fork(None, None, None, 0, None) == 1
     assert lib.kvzap_cache_pack(None, None, 1, None, None, 0, None, None, None, None) == 1
     assert lib.kvzap_cache_unpack(None, None, 1, None, None, 0, None, None, None, None) == 1
-    assert lib.kvzap_cache_share(None, None, None, 0, 8, None) == 1
+    assert lib.kvzap_cache_share(None, None, None, 0, 8, 0, None) == 1
     assert lib.kvzap_decode_attention_shared(None, None, 0, 1, None, 8, 1.0, None, None) == 1
     assert lib.kvzap_decode_attention_shared_fp8(None, None, 0, 1, None, 8, 1.0, None, None) == 1
     assert lib.kvzap_set_rotary(None, None) == 1
