@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -101,7 +102,7 @@ SIGNATURES = {
     "kvzap_decode_attention_shared": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_decode_attention_shared_fp8": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp]),
     "kvzap_set_rotary": (_i32, [_vp, ctypes.POINTER(KvzapRotaryConfig)]),
-    "kvzap_rotary": (_i32, [_vp, _vp, _i64, ctypes.POINTER(KvzapRows), _i32, _i32, _vp]),
+    "kvzap_rotary": (_i32, [_vp, _vp, _i64, _vp, _i32, _i32, _vp]),
     "kvzap_cache_lengths": (_i32, [_vp, _vp, _vp]),
     "kvzap_cache_export": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _vp]),
     "kvzap_prefill_to_cache": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _i64, _f32, _vp, _vp]),
@@ -455,9 +456,10 @@ def kvzap_set_rotary(handle, head_dim, rotary_dim, base=10000.0, interleaved=Fal
     _check(handle, load().kvzap_set_rotary(handle, ctypes.byref(cfg)))
 
 
-def rotary_rows(x, out, rotate):
-    """One tensor of kvzap_rotary: x [T, heads, D] bf16 -> out [T, heads, D] bf16 or [T, heads, D + 16] uint8 (8-bit rows); views with any
-    strides whose last dimension is contiguous."""
+_ROWS_FORMAT = ("PPqqqqiI", "PPqqqqiI" * 2, "PPqqqqiI" * 3)        # of that many KvzapRows
+
+
+def _row_fields(x, out, rotate):
     shape, out_shape, out_type = x.shape, out.shape, out.dtype
     rows8 = out_type is torch.uint8
     if len(shape) != 3 or len(out_shape) != 3 or x.dtype is not torch.bfloat16 or not (rows8 or out_type is torch.bfloat16) or \
@@ -468,14 +470,27 @@ def rotary_rows(x, out, rotate):
     at, out_at = x.stride(), out.stride()
     if not x.is_cuda or out.get_device() != x.get_device() or (some and (at[2] != 1 or out_at[2] != 1)):
         raise ValueError("rows must lie on one CUDA device, their elements side by side")
-    return KvzapRows(x.data_ptr() if some else None, out.data_ptr() if some else None, at[0], at[1], out_at[0], out_at[1], shape[1],
-                     (ROWS_ROTATE if rotate else 0) | (ROWS_8BIT if rows8 else 0))
+    return (x.data_ptr() if some else 0, out.data_ptr() if some else 0, at[0], at[1], out_at[0], out_at[1], shape[1],
+            (ROWS_ROTATE if rotate else 0) | (ROWS_8BIT if rows8 else 0))
+
+
+def rotary_rows(x, out, rotate):
+    """One tensor of kvzap_rotary: x [T, heads, D] bf16 -> out [T, heads, D] bf16 or [T, heads, D + 16] uint8 (8-bit rows); views with any
+    strides whose last dimension is contiguous."""
+    return KvzapRows(*_row_fields(x, out, rotate))
 
 
 def kvzap_rotary(handle, positions, rows, inverse=False, stream=None):
     """rows: what rotary_rows() makes of up to three tensors of the same tokens."""
     _check(handle, load().kvzap_rotary(handle, _ptr(positions), positions.shape[0], (KvzapRows * len(rows))(*rows), len(rows),
                                        1 if inverse else 0, _stream(stream)))
+
+
+def prepare_rotary(handle, positions, rows, inverse=False, stream=None) -> PreparedCall:
+    """kvzap_rotary with pre-marshalled arguments (see PreparedCall); rows: (x, out, rotate) of each tensor."""
+    args = (handle, _ptr(positions), positions.shape[0], (KvzapRows * len(rows))(*[rotary_rows(*r) for r in rows]), len(rows), 1 if inverse else 0,
+            _stream(stream))
+    return PreparedCall("kvzap_rotary", handle, args, (positions, rows))
 
 
 def kvzap_cache_lengths(handle, cache, lengths, stream=None):
@@ -633,6 +648,16 @@ def kvzap_decode_attention_fp8(handle, cache, layer_begin, layer_end, Q, scale, 
 def prepare_decode_attention_fp8(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None) -> PreparedCall:
     args = (handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O), _stream(stream))
     return PreparedCall("kvzap_decode_attention_fp8", handle, args, (Q, O))
+
+
+def prepare_decode_attention_shared(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None) -> PreparedCall:
+    args = (handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O), _stream(stream))
+    return PreparedCall("kvzap_decode_attention_shared", handle, args, (Q, O))
+
+
+def prepare_decode_attention_shared_fp8(handle, cache, layer_begin, layer_end, Q, scale, O, stream=None) -> PreparedCall:
+    args = (handle, cache, layer_begin, layer_end, _ptr(Q), Q.shape[2], scale, _ptr(O), _stream(stream))
+    return PreparedCall("kvzap_decode_attention_shared_fp8", handle, args, (Q, O))
 
 
 def prepare_decode_step(handle, cache, layer_begin, layer_end, hidden, K_new, V_new, tau, scores_out=None,
@@ -806,7 +831,7 @@ class Kvzap:
         if positions.dim() != 1 or positions.dtype != torch.int32:
             raise ValueError("positions must be int32 [T]")
         n_tokens = positions.shape[0]
-        rows, outs = [], []
+        rows, outs = (), []
         for x, out, rotate in ((Q, Q_out, True), (K, K_out, True), (V, V_out, False)):
             if x is None:
                 continue
@@ -815,11 +840,12 @@ class Kvzap:
                 raise ValueError("rows must be [%d, heads, %s], got %s" % (n_tokens, self._rotary_head_dim or "D", tuple(shape)))
             if out is None:
                 out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-            rows.append(rotary_rows(x, out, rotate))
+            rows += _row_fields(x, out, rotate)                  # packed at once: a third of the time of the structures
             outs.append(out)
-        if not rows:
+        if not outs:
             raise ValueError("rotary: no tensor given")
-        kvzap_rotary(self.handle, positions, rows, inverse, stream)
+        _check(self.handle, load().kvzap_rotary(self.handle, _ptr(positions), n_tokens, struct.pack(_ROWS_FORMAT[len(outs) - 1], *rows),
+                                                len(outs), 1 if inverse else 0, _stream(stream)))
         return outs[0] if len(outs) == 1 else tuple(outs)
 
     def create_cache(self, n_seqs, window, page_tokens, K_pool, V_pool, max_pages_per_list) -> "KvzapCache":
@@ -911,12 +937,13 @@ class KvzapCache:
         kvzap_cache_unpack(self.ctx.handle, self.handle, seqs, K, V, row_start, n_tokens, scores, stream)
 
     def _check_packed(self, n, K, V, row_start, n_tokens, scores):
-        lists = n * self.ctx.n_layers * self.ctx.n_kv_heads
-        if K.dim() != 2 or K.shape[1] != self.ctx.head_dim or K.shape != V.shape or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16:
-            raise ValueError("K and V must be bf16 [rows, %d], got %s and %s" % (self.ctx.head_dim, tuple(K.shape), tuple(V.shape)))
-        if row_start.numel() != lists + 1 or row_start.dtype != torch.int64 or n_tokens.numel() != lists or n_tokens.dtype != torch.int32:
+        ctx = self.ctx
+        lists, shape = n * ctx.n_layers * ctx.n_kv_heads, K.shape
+        if len(shape) != 2 or shape[1] != ctx.head_dim or shape != V.shape or K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
+            raise ValueError("K and V must be bf16 [rows, %d], got %s and %s" % (ctx.head_dim, tuple(shape), tuple(V.shape)))
+        if row_start.numel() != lists + 1 or row_start.dtype is not torch.int64 or n_tokens.numel() != lists or n_tokens.dtype is not torch.int32:
             raise ValueError("row_start must be int64 [%d] and n_tokens int32 [%d]" % (lists + 1, lists))
-        if scores.numel() != lists * self.window or scores.dtype != torch.float32:
+        if scores.numel() != lists * self.window or scores.dtype is not torch.float32:
             raise ValueError("scores must be fp32 [%d, %d]" % (lists, self.window))
 
     def import_prefix(self, prefix_len, page_table, next_free_page, stream=None):

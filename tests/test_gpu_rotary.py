@@ -235,6 +235,23 @@ def test_captured_and_replayed(ctx):
     assert torch.equal(out, ctx.rotary(positions, x))
 
 
+def test_prepared_call(binding, ctx):
+    ctx.set_rotary(128, 128)
+    x = torch.randn(50, 12, 128, device="cuda").bfloat16()
+    positions = torch.arange(50, dtype=torch.int32, device="cuda")
+    Q, K, V = x[:, :8], x[:, 8:10], x[:, 10:]
+    want = ctx.rotary(positions, Q, K, V)
+    got = [torch.empty_like(w) for w in want]
+    call = binding.prepare_rotary(ctx.handle, positions, [(Q, got[0], True), (K, got[1], True), (V, got[2], False)])
+    call()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    positions += 1
+    call()
+    assert all(torch.equal(a, b) for a, b in zip(got, ctx.rotary(positions, Q, K, V)))
+    binding.kvzap_rotary(ctx.handle, positions, [binding.rotary_rows(Q, got[0], True)], inverse=True)
+    assert torch.equal(got[0], ctx.rotary(positions, Q, inverse=True))
+
+
 def test_refusals(binding, ctx):
     fresh = binding.Kvzap(64, 0, 2, 128, 1, max_tokens=64)
     x = torch.zeros(4, 2, 128, dtype=torch.bfloat16, device="cuda")

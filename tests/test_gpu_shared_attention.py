@@ -628,3 +628,19 @@ def test_little_to_save_is_read_by_itself(binding):
     assert [launches([0]), launches([1]), launches([2]), launches([0, 1, 2])] == [1, 2, 1, 2]
     s.cache.share([list(range(12))], 32)
     assert [launches([0]), launches([1]), launches([2])] == [2, 2, 2]
+
+
+@pytest.mark.parametrize("rows8", [False, True])
+def test_prepared_call(binding, rows8):
+    s = (Setup8 if rows8 else Setup)(binding, 4, 2, 2, 64, 0, 16, 40, n_pages=1000, seed=31)
+    s.fill(0, [500, 0, 300, 129])
+    s.cache.fork([0, 0, 0], [1, 2, 3])
+    s.cache.share([[0, 1, 2, 3]], 8)
+    Q = torch.randn(2, 4, 8, 64, device="cuda").bfloat16()
+    want, got = torch.empty_like(Q), torch.empty_like(Q)
+    name = "decode_attention_shared_fp8" if rows8 else "decode_attention_shared"
+    getattr(binding, "kvzap_" + name)(s.ctx.handle, s.cache.handle, 0, 2, Q, 0.125, want)
+    before = s.ctx.launch_count()
+    getattr(binding, "prepare_" + name)(s.ctx.handle, s.cache.handle, 0, 2, Q, 0.125, got)()
+    assert s.ctx.launch_count() == before + 2
+    assert torch.equal(got, want)
